@@ -59,6 +59,99 @@ struct rpo_batch;
 int rpo_attn_decode(struct rpo_batch *b, int32_t layer, const void *q_dev, int32_t n_rows, int32_t n_suffix,
                     const uint8_t *active_dev, void *out_dev, void *stream);
 
+/* ---- a paged cache outside a batch ---------------------------------------------------------------
+ * Keys and values of n_seqs sequences in pages of one layer: what a batch keeps, as building blocks for caches whose size is
+ * bounded (a sliding window with sinks, or eviction by accumulated attention weight).
+ * Page p of the pool starts p * page_stride elements in and holds, for every KV head, a key block [page_tokens][head_dim],
+ * then for every KV head a value block [page_tokens / 8][head_dim][8] (eight tokens of a channel side by side).  The slots
+ * [k * page_tokens, (k + 1) * page_tokens) of sequence s lie in page table_dev[s * table_stride + k]; slots are numbered from 0
+ * without a gap, whatever positions the tokens had, and keys lie in the cache as they are multiplied (already rotated).
+ *   pool_dev      device, 16-byte aligned; page_stride >= 2 * n_kv_heads * page_tokens * head_dim, a multiple of 8
+ *   table_dev     device int32 [n_seqs, table_stride]; table_stride * page_tokens at most 2^30
+ *   len_dev       device int32 [n_seqs]: slots in use.  What lies in other slots does not matter, NaN included
+ *   n_seqs at most 65535; page_tokens a power of two, >= 16; head_dim even, <= 256; dtype RPO_F32 or RPO_BF16
+ * What lies on the device cannot be checked on the host.  Every index from there is bounded by the kernels: a table entry
+ * outside [0, n_pages) means that its tokens are not there (not visible, neither read nor written), a length counts up to
+ * table_stride * page_tokens, row ranges end with the row arrays.  Several sequences may share pages that are only read. */
+typedef struct {
+    void *pool_dev;
+    const int32_t *table_dev;
+    const int32_t *len_dev;
+    int64_t page_stride;
+    int32_t n_pages, n_seqs, table_stride, page_tokens, n_kv_heads, head_dim, dtype;
+} rpo_paged_kv;
+
+/* One layer of a forked batch as such a cache: its pool and the page tables of its n_groups * G rollouts, where position =
+ * slot.  len_dev is left NULL for the caller to fill in (prefix_len + tokens appended per rollout).  The rollouts of a group
+ * share their prefix pages: do not append below prefix_len.  Host only.  Errors: RPO_ESTATE unless forked; RPO_EINVAL. */
+int rpo_batch_kv(const struct rpo_batch *b, int32_t layer, rpo_paged_kv *out);
+
+/* The rows of a call (below): sequence s has rows cu_rows_dev[s] .. cu_rows_dev[s + 1] - 1 of the row arrays, any number from
+ * 0 up to max_new (the longest; a host bound that sizes the launch: rows of a sequence beyond it are not looked at).  They
+ * are the last tokens of its cache: with n rows, row i sits at slot len - n + i.  cu_rows_dev: device int32 [n_seqs + 1],
+ * not decreasing.  Rows of the arrays that belong to no sequence are left as they were.
+ *
+ * rpo_kv_append: write the rows' keys and values into their slots (len_dev counts them already).
+ *   k_dev, v_dev  device, n_rows rows of n_kv_heads * head_dim values, k_stride / v_stride elements apart
+ * Rows that would lie below slot 0 or beyond the table are dropped.  Errors: RPO_EINVAL, RPO_EHIP. */
+int rpo_kv_append(const rpo_paged_kv *kv, const void *k_dev, int64_t k_stride, const void *v_dev, int64_t v_stride,
+                  const int32_t *cu_rows_dev, int32_t n_rows, int32_t max_new, void *stream);
+
+/* Attention of the rows over their sequences' caches, single tokens and whole chunks alike: query head h of a row at slot t
+ * reads KV head h / (n_q_heads / n_kv_heads) and sees the slots j <= t, with a window only those of them with j < n_sinks or
+ * j > t - window.  out = softmax(scale q k^T) v over what it sees; zeros where it sees nothing.
+ *   q_dev       device, n_rows rows of n_q_heads * head_dim values (head h at column h * head_dim), q_stride elements apart
+ *   max_len     no cache is longer (host; chooses how the work is split)
+ *   window      0: all earlier slots; n_sinks counts only with a window
+ *   out_dev     device, like q_dev with out_stride; must not overlap q_dev
+ *   lse_out_dev device fp32 [n_rows, n_q_heads] or NULL: ln sum exp(scale q k^T), -infinity where nothing is seen
+ *   ws_dev      device, 16-byte aligned, at least rpo_attn_paged_ws_bytes for the same arguments, or NULL / 0: the tokens of
+ *               a sequence are then not split (few rows over long caches are slower).  Nothing in it needs clearing; calls
+ *               that may run at the same time (captured graphs among them) need one each.
+ * bf16 and fp32 with head_dim 32, 64 or 128 and rows that start at multiples of 16 bytes run on the matrix cores, anything
+ * else on a generic kernel.  Sums and statistics are fp32; with bf16 the weights p are rounded to bf16 before they multiply
+ * the values, as in the batch's attention.  A NaN or infinity in a slot reaches the rows that see it and may reach the rows
+ * of the same sequence that are computed together with them; in slots that no row of the call sees it does nothing.
+ * Errors: RPO_EINVAL, RPO_ENOMEM (ws_bytes), RPO_EHIP. */
+size_t rpo_attn_paged_ws_bytes(const rpo_paged_kv *kv, int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads,
+                               int32_t window, int32_t n_sinks);
+int rpo_attn_paged(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, const int32_t *cu_rows_dev, int32_t n_rows,
+                   int32_t max_new, int32_t max_len, int32_t n_q_heads, float scale, int32_t window, int32_t n_sinks,
+                   void *out_dev, int64_t out_stride, float *lse_out_dev, void *ws_dev, size_t ws_bytes, void *stream);
+
+/* Attention weight that the cached tokens receive from the rows: for every slot j < len of every KV head
+ *   score_out = score_in + sum over rows and the head's query heads that see j of exp(scale q k_j - lse)
+ * lse_dev device fp32 [n_rows, n_q_heads]: what rpo_attn_paged left for the same rows (a row with -infinity gives nothing).
+ *   score_in_dev  device fp32 [n_seqs, n_kv_heads, score_stride] or NULL: zeros; score_out_dev the same layout, may be the
+ *                 same array.  score_stride >= the longest cache (slots beyond it get no score); slots from len on are left
+ *                 as they were.  The sums run in a fixed order: equal inputs give equal bits.
+ *   ws_dev        as for rpo_attn_paged, rpo_kv_score_ws_bytes long
+ * The other arguments as for rpo_attn_paged; slots from max_len on get no score.  Errors: RPO_EINVAL, RPO_ENOMEM, RPO_EHIP. */
+size_t rpo_kv_score_ws_bytes(const rpo_paged_kv *kv, int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads,
+                             int32_t window, int32_t n_sinks);
+int rpo_kv_score(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, const int32_t *cu_rows_dev, int32_t n_rows,
+                 int32_t max_new, int32_t max_len, int32_t n_q_heads, float scale, int32_t window, int32_t n_sinks,
+                 const float *lse_dev, const float *score_in_dev, float *score_out_dev, int64_t score_stride, void *ws_dev,
+                 size_t ws_bytes, void *stream);
+
+/* Evict what was attended to least: every sequence that holds more than `budget` tokens keeps, per KV head, its first
+ * n_sinks and its last n_recent slots and of the others the budget - n_sinks - n_recent with the highest scores (ties: the
+ * lower slot; NaN below every number).  What is kept goes, in order, to slots 0 .. of `dst`: other pages, so that pages
+ * which other sequences share stay as they are.  A shorter sequence goes over whole.
+ *   score_dev     device fp32 [n_seqs, n_kv_heads, score_stride], score_stride >= the longest cache (tokens beyond it are
+ *                 not looked at)
+ *   budget        >= 1, >= n_sinks + n_recent, at most what a row of dst's table holds
+ *   dst           same n_seqs, n_kv_heads, head_dim and dtype as src; its len_dev is not read and may be NULL; no page that
+ *                 its tables name may be one that src's name.  Slots beyond the kept ones are left as they were
+ *   len_out_dev   device int32 [n_seqs]: min(len, budget); may be src's or dst's len_dev
+ *   score_out_dev device fp32 [n_seqs, n_kv_heads, score_out_stride] or NULL, score_out_stride >= budget, not score_dev: the
+ *                 kept tokens' scores, 0 in the rest of the row
+ *   kept_out_dev  device int32 [n_seqs, n_kv_heads, budget]: the old slot of every new one, -1 beyond the length
+ * Errors: RPO_EINVAL, RPO_EHIP. */
+int rpo_kv_evict(const rpo_paged_kv *src, const float *score_dev, int64_t score_stride, int32_t budget, int32_t n_sinks,
+                 int32_t n_recent, const rpo_paged_kv *dst, int32_t *len_out_dev, float *score_out_dev,
+                 int64_t score_out_stride, int32_t *kept_out_dev, void *stream);
+
 /* rpo_gemm_nt for callers that cannot allocate or pass a workspace (code under HIP graph capture,
  * tight serving loops, harnesses that forbid hipMalloc): the same contraction, kernels and
  * results, with the K-split partial sums in a fixed 16 MiB device array that belongs to the

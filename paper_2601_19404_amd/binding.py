@@ -38,6 +38,13 @@ class Weights(C.Structure):
                 ("w_gate_up", C.POINTER(C.c_void_p)), ("w_down", C.POINTER(C.c_void_p))]
 
 
+class PagedKvDesc(C.Structure):
+    _fields_ = [("pool_dev", C.c_void_p), ("table_dev", C.c_void_p), ("len_dev", C.c_void_p),
+                ("page_stride", C.c_int64), ("n_pages", C.c_int32), ("n_seqs", C.c_int32),
+                ("table_stride", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
 _lib = None
 
 
@@ -79,6 +86,16 @@ def lib() -> C.CDLL:
     L.rpo_gemm_nt.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, sz, vp]
     L.rpo_gemm_nt_noalloc.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp]
     L.rpo_gemm_plan.argtypes = [i32, i32, i32, i32, i32, sz, sz, C.POINTER(i32)]
+    kv = C.POINTER(PagedKvDesc)
+    L.rpo_batch_kv.argtypes = [vp, i32, kv]
+    L.rpo_kv_append.argtypes = [kv, vp, i64, vp, i64, vp, i32, i32, vp]
+    L.rpo_attn_paged_ws_bytes.argtypes = [kv, i32, i32, i32, i32, i32, i32]
+    L.rpo_attn_paged_ws_bytes.restype = sz
+    L.rpo_attn_paged.argtypes = [kv, vp, i64, vp, i32, i32, i32, i32, f32, i32, i32, vp, i64, vp, vp, sz, vp]
+    L.rpo_kv_score_ws_bytes.argtypes = [kv, i32, i32, i32, i32, i32, i32]
+    L.rpo_kv_score_ws_bytes.restype = sz
+    L.rpo_kv_score.argtypes = [kv, vp, i64, vp, i32, i32, i32, i32, f32, i32, i32, vp, vp, vp, i64, vp, sz, vp]
+    L.rpo_kv_evict.argtypes = [kv, vp, i64, i32, i32, i32, kv, vp, vp, i64, vp, vp]
     L.rpo_probe_peaks.argtypes = [vp, vp, sz, vp, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]
     L.rpo_set_kernel_path.argtypes = [C.c_int]
     L.rpo_profile_start.argtypes = [C.c_int, C.c_int]
@@ -87,7 +104,8 @@ def lib() -> C.CDLL:
     for name in ("rpo_model_create", "rpo_batch_create", "rpo_prefill_prefix", "rpo_kv_fork",
                  "rpo_decode_step", "rpo_decode_step_compact", "rpo_sample", "rpo_suffix_logprobs", "grpo_advantages",
                  "rpo_shape_rewards", "rpo_objective_forward", "rpo_cut_pack", "rpo_cache_update", "rpo_gemm_nt",
-                 "rpo_attn_decode", "rpo_gemm_nt_noalloc", "rpo_gemm_plan", "rpo_set_kernel_path", "rpo_profile_start", "rpo_profile_stop", "rpo_probe_peaks"):
+                 "rpo_attn_decode", "rpo_gemm_nt_noalloc", "rpo_gemm_plan", "rpo_set_kernel_path", "rpo_profile_start", "rpo_profile_stop", "rpo_probe_peaks",
+                 "rpo_batch_kv", "rpo_kv_append", "rpo_attn_paged", "rpo_kv_score", "rpo_kv_evict"):
         getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -97,7 +115,8 @@ EXPORTS = ("rpo_model_create", "rpo_model_destroy", "rpo_kv_pool_bytes", "rpo_wo
            "rpo_batch_create", "rpo_batch_destroy", "rpo_prefill_prefix", "rpo_kv_fork",
            "rpo_decode_step", "rpo_decode_step_compact", "rpo_sample", "rpo_suffix_logprobs", "grpo_advantages",
            "rpo_shape_rewards", "rpo_objective_forward", "rpo_cut_pack", "rpo_cache_update", "rpo_last_error", "rpo_gemm_nt", "rpo_attn_decode", "rpo_gemm_nt_noalloc", "rpo_gemm_plan", "rpo_set_kernel_path", "rpo_profile_start",
-           "rpo_profile_stop", "rpo_probe_peaks")
+           "rpo_profile_stop", "rpo_probe_peaks", "rpo_batch_kv", "rpo_kv_append", "rpo_attn_paged_ws_bytes",
+           "rpo_attn_paged", "rpo_kv_score_ws_bytes", "rpo_kv_score", "rpo_kv_evict")
 
 
 def _check(code: int) -> None:
@@ -386,6 +405,181 @@ def rpo_attn_decode(batch: Batch, layer: int, q_dev: torch.Tensor, n_rows: int, 
         raise ValueError("q_dev / out_dev smaller than n_rows x n_q_heads x head_dim")
     _check(lib().rpo_attn_decode(batch.handle, layer, q_dev.data_ptr(), n_rows, n_suffix, _ptr(active_dev),
                                  out_dev.data_ptr(), _stream(stream)))
+
+
+# ---- a paged cache outside a batch ------------------------------------------
+class PagedKV:
+    """rpo_paged_kv over tensors: pool [n_pages, ...] (float32 or bfloat16, a page's elements side by side), table
+    [n_seqs, pages of a sequence] int32, lens [n_seqs] int32.  Keeps the tensors alive; `desc` holds their addresses, so
+    lengths are updated in place."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page_tokens: int, n_kv_heads: int,
+                 head_dim: int):
+        if pool.dtype not in (torch.float32, torch.bfloat16) or not pool.is_cuda or pool.dim() < 2 \
+                or not pool[:1].is_contiguous():
+            raise ValueError("pool: need a float32 or bfloat16 device tensor [n_pages, ...], contiguous within a page")
+        _dev(table, torch.int32, "table")
+        _dev(lens, torch.int32, "lens")
+        if table.dim() != 2 or lens.numel() < table.shape[0]:
+            raise ValueError("table must be 2-D, lens [n_seqs]")
+        if pool[0].numel() < 2 * n_kv_heads * page_tokens * head_dim:
+            raise ValueError("pool: a page is shorter than 2 x n_kv_heads x page_tokens x head_dim")
+        if not pool.device == table.device == lens.device:
+            raise ValueError("pool, table and lens lie on different devices")
+        self.pool, self.table, self.lens = pool, table, lens
+        self.desc = PagedKvDesc(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), pool.stride(0), pool.shape[0],
+                                table.shape[0], table.shape[1], page_tokens, n_kv_heads, head_dim,
+                                RPO_F32 if pool.dtype == torch.float32 else RPO_BF16)
+        self.capacity = table.shape[1] * page_tokens     # tokens that a row of the table holds
+        self.device = pool.device
+
+    @classmethod
+    def of_batch(cls, batch: Batch, layer: int, lens: torch.Tensor) -> "PagedKV":
+        """One layer of a forked batch; lens [n_groups * G] int32: tokens of every rollout."""
+        self = cls.__new__(cls)
+        self.desc = PagedKvDesc()
+        _check(lib().rpo_batch_kv(batch.handle, layer, C.byref(self.desc)))
+        _dev(lens, torch.int32, "lens")
+        if lens.numel() < self.desc.n_seqs or lens.device != batch.kv_pool.device:
+            raise ValueError("lens: need n_groups * G lengths on the batch's device")
+        self.desc.len_dev = lens.data_ptr()
+        self.batch, self.pool, self.table, self.lens = batch, batch.kv_pool, None, lens
+        self.capacity = self.desc.table_stride * self.desc.page_tokens
+        self.device = lens.device
+        return self
+
+
+def _on(kv: PagedKV, stream, **tensors) -> int:
+    """The stream to launch on; every tensor has to lie on the cache's device, and the stream too."""
+    if stream is None:
+        stream = torch.cuda.current_stream(kv.device)
+    elif stream.device != kv.device:
+        raise ValueError("the stream belongs to another device than the cache")
+    if kv.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache lies on {kv.device}, which is not the current device")
+    for name, t in tensors.items():
+        if t is not None and t.device != kv.device:
+            raise ValueError(f"{name} lies on another device than the cache")
+    return stream.cuda_stream
+
+
+def _rows(t: torch.Tensor, kv: PagedKV, width: int, name: str) -> torch.Tensor:
+    dt = torch.float32 if kv.desc.dtype == RPO_F32 else torch.bfloat16
+    if t.dim() != 2 or t.dtype != dt or t.shape[1] != width or (t.shape[0] > 1 and t.stride(0) < width) \
+            or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: need {dt} rows of {width} values with unit column stride")
+    return t
+
+
+def _stride(t: torch.Tensor) -> int:
+    return max(t.stride(0), t.shape[1])
+
+
+def _cu(cu_rows_dev: torch.Tensor, kv: PagedKV) -> torch.Tensor:
+    _dev(cu_rows_dev, torch.int32, "cu_rows_dev")
+    if cu_rows_dev.numel() < kv.desc.n_seqs + 1:
+        raise ValueError("cu_rows_dev: need n_seqs + 1 values")
+    return cu_rows_dev
+
+
+def _q_heads(q_dev: torch.Tensor, kv: PagedKV) -> int:
+    n, rest = divmod(q_dev.shape[-1], kv.desc.head_dim)
+    if rest:
+        raise ValueError("q_dev: a row is not a whole number of heads")
+    return n
+
+
+def _score_rows(t, kv: PagedKV, name: str, at_least: int = 1):
+    if t is not None:
+        _dev(t, torch.float32, name)
+        if tuple(t.shape[:-1]) != (kv.desc.n_seqs, kv.desc.n_kv_heads) or t.shape[-1] < at_least:
+            raise ValueError(f"{name}: need [n_seqs, n_kv_heads, at least {at_least}]")
+    return t
+
+
+def rpo_kv_append(kv: PagedKV, k_dev: torch.Tensor, v_dev: torch.Tensor, cu_rows_dev: torch.Tensor, max_new: int,
+                  stream=None) -> None:
+    """Write the rows' keys and values [n_rows, n_kv_heads * head_dim] to the last slots of their sequences."""
+    width = kv.desc.n_kv_heads * kv.desc.head_dim
+    _rows(k_dev, kv, width, "k_dev")
+    _rows(v_dev, kv, width, "v_dev")
+    _cu(cu_rows_dev, kv)
+    if k_dev.shape[0] != v_dev.shape[0]:
+        raise ValueError("k_dev and v_dev differ in rows")
+    on = _on(kv, stream, k_dev=k_dev, v_dev=v_dev, cu_rows_dev=cu_rows_dev)
+    _check(lib().rpo_kv_append(C.byref(kv.desc), k_dev.data_ptr(), _stride(k_dev), v_dev.data_ptr(), _stride(v_dev),
+                               cu_rows_dev.data_ptr(), k_dev.shape[0], max_new, on))
+
+
+def rpo_attn_paged_ws_bytes(kv: PagedKV, n_rows: int, max_new: int, max_len: int, n_q_heads: int, window: int = 0,
+                            n_sinks: int = 0) -> int:
+    return lib().rpo_attn_paged_ws_bytes(C.byref(kv.desc), n_rows, max_new, max_len, n_q_heads, window, n_sinks)
+
+
+def rpo_attn_paged(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, max_new: int, out_dev: torch.Tensor,
+                   window: int = 0, n_sinks: int = 0, scale: float | None = None, lse_out_dev=None, ws_dev=None,
+                   max_len: int | None = None, stream=None) -> None:
+    """Attention of rows [n_rows, n_q_heads * head_dim] over their sequences' pages.  scale: 1 / sqrt(head_dim) if not
+    given; max_len: what the table holds if not given; ws_dev: uint8, rpo_attn_paged_ws_bytes long."""
+    Hq = _q_heads(q_dev, kv)
+    _rows(q_dev, kv, q_dev.shape[1], "q_dev")
+    _rows(out_dev, kv, q_dev.shape[1], "out_dev")
+    _cu(cu_rows_dev, kv)
+    if out_dev.shape[0] != q_dev.shape[0]:
+        raise ValueError("out_dev and q_dev differ in rows")
+    if lse_out_dev is not None and _dev(lse_out_dev, torch.float32, "lse_out_dev").numel() < q_dev.shape[0] * Hq:
+        raise ValueError("lse_out_dev smaller than n_rows x n_q_heads")
+    on = _on(kv, stream, q_dev=q_dev, out_dev=out_dev, cu_rows_dev=cu_rows_dev, lse_out_dev=lse_out_dev, ws_dev=ws_dev)
+    _check(lib().rpo_attn_paged(C.byref(kv.desc), q_dev.data_ptr(), _stride(q_dev), cu_rows_dev.data_ptr(),
+                                q_dev.shape[0], max_new, kv.capacity if max_len is None else max_len, Hq,
+                                kv.desc.head_dim ** -0.5 if scale is None else scale, window, n_sinks,
+                                out_dev.data_ptr(), _stride(out_dev), _ptr(lse_out_dev), _ptr(ws_dev),
+                                0 if ws_dev is None else ws_dev.numel() * ws_dev.element_size(), on))
+
+
+def rpo_kv_score_ws_bytes(kv: PagedKV, n_rows: int, max_new: int, max_len: int, n_q_heads: int, window: int = 0,
+                          n_sinks: int = 0) -> int:
+    return lib().rpo_kv_score_ws_bytes(C.byref(kv.desc), n_rows, max_new, max_len, n_q_heads, window, n_sinks)
+
+
+def rpo_kv_score(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, max_new: int, lse_dev: torch.Tensor,
+                 score_in_dev, score_out_dev: torch.Tensor, window: int = 0, n_sinks: int = 0, scale: float | None = None,
+                 ws_dev=None, max_len: int | None = None, stream=None) -> None:
+    """score_out = score_in (None: zeros) + the attention weight that every cached token receives from the rows."""
+    Hq = _q_heads(q_dev, kv)
+    _rows(q_dev, kv, q_dev.shape[1], "q_dev")
+    _cu(cu_rows_dev, kv)
+    if _dev(lse_dev, torch.float32, "lse_dev").numel() < q_dev.shape[0] * Hq:
+        raise ValueError("lse_dev smaller than n_rows x n_q_heads")
+    _score_rows(score_out_dev, kv, "score_out_dev")
+    _score_rows(score_in_dev, kv, "score_in_dev")
+    if score_in_dev is not None and score_in_dev.shape != score_out_dev.shape:
+        raise ValueError("score_in_dev and score_out_dev differ in shape")
+    on = _on(kv, stream, q_dev=q_dev, cu_rows_dev=cu_rows_dev, lse_dev=lse_dev, score_in_dev=score_in_dev,
+             score_out_dev=score_out_dev, ws_dev=ws_dev)
+    _check(lib().rpo_kv_score(C.byref(kv.desc), q_dev.data_ptr(), _stride(q_dev), cu_rows_dev.data_ptr(),
+                              q_dev.shape[0], max_new, kv.capacity if max_len is None else max_len, Hq,
+                              kv.desc.head_dim ** -0.5 if scale is None else scale, window, n_sinks, lse_dev.data_ptr(),
+                              _ptr(score_in_dev), score_out_dev.data_ptr(), score_out_dev.shape[-1], _ptr(ws_dev),
+                              0 if ws_dev is None else ws_dev.numel() * ws_dev.element_size(), on))
+
+
+def rpo_kv_evict(kv: PagedKV, score_dev: torch.Tensor, budget: int, n_sinks: int, n_recent: int, dst: PagedKV,
+                 len_out_dev: torch.Tensor, kept_out_dev: torch.Tensor, score_out_dev=None, stream=None) -> None:
+    """Keep `budget` tokens per KV head of every longer sequence; the kept ones go to dst's pages."""
+    _score_rows(score_dev, kv, "score_dev")
+    _score_rows(score_out_dev, kv, "score_out_dev", max(budget, 1))
+    _dev(len_out_dev, torch.int32, "len_out_dev")
+    _dev(kept_out_dev, torch.int32, "kept_out_dev")
+    if len_out_dev.numel() < kv.desc.n_seqs or kept_out_dev.numel() < kv.desc.n_seqs * kv.desc.n_kv_heads * budget:
+        raise ValueError("len_out_dev / kept_out_dev smaller than n_seqs / n_seqs x n_kv_heads x budget")
+    if dst.device != kv.device:
+        raise ValueError("src and dst lie on different devices")
+    on = _on(kv, stream, score_dev=score_dev, len_out_dev=len_out_dev, kept_out_dev=kept_out_dev,
+             score_out_dev=score_out_dev)
+    _check(lib().rpo_kv_evict(C.byref(kv.desc), score_dev.data_ptr(), score_dev.shape[-1], budget, n_sinks, n_recent,
+                              C.byref(dst.desc), len_out_dev.data_ptr(), _ptr(score_out_dev),
+                              0 if score_out_dev is None else score_out_dev.shape[-1], kept_out_dev.data_ptr(), on))
 
 
 def rpo_gemm_nt_noalloc(a_dev: torch.Tensor, w_dev: torch.Tensor, c_dev: torch.Tensor, epilogue: int,

@@ -322,4 +322,96 @@ hipError_t launch_compact_rows(const uint8_t* active, int n_rows, int32_t* live,
 hipError_t launch_advantages(const float* rewards, int n_groups, int G, int ddof, float eps, float* adv,
                              hipStream_t s);
 
+// ---- operators of a paged cache outside a batch (paged_cache.hip, paged_attention.hip) ----------
+// One layer's pages with the tables and lengths of n_seqs sequences, laid out as KvGeom's of one layer.  Lengths, tables
+// and row counts lie on the device, where the host cannot check them: the kernels bound every index they take from them
+// (tokens of a page outside the pool are not there, a length ends with the table, row ranges with the row arrays).
+struct PagedKv {
+    void* pool;
+    const int32_t* table;  // [n_seqs, table_stride]
+    const int32_t* len;    // [n_seqs]
+    int64_t page_stride;   // elements
+    int n_pages, n_seqs, table_stride;
+    int shift;             // log2(tokens of a page)
+    int Hkv, dh, dtype;
+    __host__ __device__ int64_t block() const { return (int64_t)dh << shift; }
+    __device__ int length(int s) const {
+        const int cap = table_stride << shift;
+        return min(max(len[s], 0), cap);
+    }
+    // page of a slot below the table's end, -1 if it is not one of the pool's
+    __device__ int page(int s, int slot) const {
+        const int p = table[(int64_t)s * table_stride + (slot >> shift)];
+        return (unsigned)p < (unsigned)n_pages ? p : -1;
+    }
+    __device__ int64_t k_at(int page, int h) const { return page * page_stride + h * block(); }
+    __device__ int64_t v_at(int page, int h) const { return page * page_stride + (Hkv + h) * block(); }
+};
+
+// The rows of one sequence in a call: rows [row0, row0 + n) of the row arrays, row i at slot slot0 + i of the cache (below
+// 0 where the call has more rows than the cache has tokens).
+struct ChunkRows {
+    int row0, n, slot0;
+};
+__device__ inline ChunkRows chunk_rows(const PagedKv& kv, const int32_t* cu, int s, int n_rows, int max_new) {
+    const int64_t a = cu[s], b = cu[s + 1];
+    const int64_t all = b > a ? (b - a < 0x7fffffff ? b - a : 0x7fffffff) : 0;
+    const int64_t end = b < n_rows ? b : n_rows;
+    ChunkRows c;
+    c.row0 = (int)(a > 0 ? a : 0);
+    int64_t n = a < 0 ? 0 : (end - a < max_new ? end - a : max_new);
+    c.n = n > 0 ? (int)n : 0;
+    c.slot0 = (int)(kv.length(s) - all);
+    return c;
+}
+
+struct PagedAppendArgs {
+    PagedKv kv;
+    const void *k, *v;
+    int64_t k_stride, v_stride;  // elements
+    const int32_t* cu;
+    int n_rows, max_new;
+};
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s);
+
+struct PagedEvictArgs {
+    PagedKv src, dst;
+    const float* score;  // [n_seqs, Hkv, score_stride]
+    int64_t score_stride;
+    int budget, sinks, recent;
+    int32_t* len_out;    // [n_seqs]
+    float* score_out;    // [n_seqs, Hkv, score_out_stride] or NULL
+    int64_t score_out_stride;
+    int32_t* kept;       // [n_seqs, Hkv, budget]
+};
+hipError_t launch_paged_evict(const PagedEvictArgs& a, hipStream_t s);
+
+struct PagedAttnArgs {
+    PagedKv kv;
+    const void* q;  // [n_rows, q_stride], head h at column h * dh
+    int64_t q_stride;
+    const int32_t* cu;
+    int n_rows, max_new, max_len, Hq;
+    float scale;
+    int window, sinks;  // window 0: none
+    void* out;          // [n_rows, out_stride]
+    int64_t out_stride;
+    float* lse;         // [n_rows, Hq] natural logarithm, or NULL
+    void* ws;           // partial results of a split over the tokens, or NULL: not split
+    size_t ws_bytes;
+    int path;           // as in AttnArgs
+};
+hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
+size_t paged_attn_ws_bytes(const PagedAttnArgs& a);  // pointers are not looked at
+
+struct PagedScoreArgs {
+    PagedAttnArgs at;        // out, lse unused
+    const float* lse_in;     // [n_rows, Hq]
+    const float* score_in;   // [n_seqs, Hkv, score_stride] or NULL: zeros
+    float* score_out;        // the same layout
+    int64_t score_stride;
+};
+hipError_t launch_paged_score(const PagedScoreArgs& a, hipStream_t s);
+size_t paged_score_ws_bytes(const PagedScoreArgs& a);
+
 }  // namespace rpo

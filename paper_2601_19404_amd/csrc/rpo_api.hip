@@ -1242,3 +1242,224 @@ extern "C" int rpo_gemm_nt_noalloc(const void* a_dev, int64_t lda, const void* w
     HIP_TRY(launch_gemm(g, (hipStream_t)stream));
     return RPO_OK;
 }
+
+// ---------------------------------------------------------------------------
+// a paged cache outside a batch
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int kMaxSeqs = 65535;  // grid dimensions y and z
+
+// The checks of a cache that the host can make; fills in the kernels' form of it.
+int paged_kv(const char* who, const rpo_paged_kv* kv, bool needs_len, PagedKv* o) {
+    if (!kv) return fail(RPO_EINVAL, "%s: NULL cache", who);
+    if (!kv->pool_dev || !kv->table_dev || (needs_len && !kv->len_dev)) return fail(RPO_EINVAL, "%s: NULL pointer in a cache", who);
+    if (kv->dtype != RPO_F32 && kv->dtype != RPO_BF16) return fail(RPO_EINVAL, "%s: unknown dtype %d", who, kv->dtype);
+    if (kv->n_seqs < 0 || kv->n_seqs > kMaxSeqs || kv->n_pages < 1 || kv->table_stride < 1 || kv->n_kv_heads < 1 ||
+        kv->n_kv_heads > 1024)
+        return fail(RPO_EINVAL, "%s: bad sizes of a cache (n_seqs 0..%d, n_kv_heads 1..1024)", who, kMaxSeqs);
+    if (kv->head_dim < 2 || kv->head_dim > 256 || kv->head_dim % 2)
+        return fail(RPO_EINVAL, "%s: head_dim must be even and <= 256", who);
+    const int pt = kv->page_tokens;
+    if (pt < 16 || (pt & (pt - 1))) return fail(RPO_EINVAL, "%s: page_tokens must be a power of two >= 16", who);
+    if ((int64_t)kv->table_stride * pt > ((int64_t)1 << 30))
+        return fail(RPO_EINVAL, "%s: table_stride * page_tokens must be at most 2^30", who);
+    if (kv->page_stride < (int64_t)2 * kv->n_kv_heads * pt * kv->head_dim || kv->page_stride % 8)
+        return fail(RPO_EINVAL, "%s: page_stride must hold a page and be a multiple of 8", who);
+    if ((uintptr_t)kv->pool_dev % 16) return fail(RPO_EINVAL, "%s: the pool must be 16-byte aligned", who);
+    o->pool = kv->pool_dev;
+    o->table = kv->table_dev;
+    o->len = kv->len_dev;
+    o->page_stride = kv->page_stride;
+    o->n_pages = kv->n_pages;
+    o->n_seqs = kv->n_seqs;
+    o->table_stride = kv->table_stride;
+    o->shift = 0;
+    while ((1 << o->shift) < pt) ++o->shift;
+    o->Hkv = kv->n_kv_heads;
+    o->dh = kv->head_dim;
+    o->dtype = kv->dtype;
+    return RPO_OK;
+}
+
+int rows_args(const char* who, const int32_t* cu, int n_rows, int max_new) {
+    if (!cu) return fail(RPO_EINVAL, "%s: NULL argument", who);
+    if (n_rows < 0 || n_rows > (1 << 30) || max_new < 0 || max_new > n_rows)
+        return fail(RPO_EINVAL, "%s: need 0 <= max_new <= n_rows <= 2^30", who);
+    return RPO_OK;
+}
+
+// What rpo_attn_paged and rpo_kv_score have in common.
+int attn_args(const char* who, const rpo_paged_kv* kv, int n_rows, int max_new, int max_len, int Hq, int window, int sinks,
+              PagedAttnArgs* a) {
+    const int rc = paged_kv(who, kv, true, &a->kv);
+    if (rc != RPO_OK) return rc;
+    if (Hq < 1 || Hq > 65535 || Hq % a->kv.Hkv) return fail(RPO_EINVAL, "%s: n_q_heads must be a multiple of n_kv_heads, <= 65535", who);
+    if (n_rows < 0 || max_new < 0 || max_new > n_rows || n_rows > (1 << 30) || (int64_t)max_new * (Hq / a->kv.Hkv) > (1 << 30))
+        return fail(RPO_EINVAL, "%s: need 0 <= max_new <= n_rows, and n_rows and max_new * n_q_heads / n_kv_heads <= 2^30", who);
+    if (max_len < 0) return fail(RPO_EINVAL, "%s: max_len must be >= 0", who);
+    if (window < 0 || sinks < 0) return fail(RPO_EINVAL, "%s: window and n_sinks must be >= 0", who);
+    const int64_t cap = (int64_t)a->kv.table_stride << a->kv.shift;
+    a->n_rows = n_rows;
+    a->max_new = max_new;
+    a->max_len = (int)std::min((int64_t)max_len, cap);
+    a->Hq = Hq;
+    a->window = window;
+    a->sinks = window ? (int)std::min((int64_t)sinks, cap) : 0;
+    a->q = nullptr;
+    a->q_stride = a->out_stride = (int64_t)Hq * a->kv.dh;
+    a->cu = nullptr;
+    a->scale = 1.f;
+    a->out = nullptr;
+    a->lse = nullptr;
+    a->ws = nullptr;
+    a->ws_bytes = 0;
+    a->path = g_kernel_path;
+    return RPO_OK;
+}
+
+int attn_pointers(const char* who, PagedAttnArgs* a, const void* q, int64_t q_stride, const int32_t* cu, float scale, void* ws,
+                  size_t ws_bytes) {
+    if (!cu || (!q && a->n_rows > 0)) return fail(RPO_EINVAL, "%s: NULL argument", who);
+    if (q_stride < (int64_t)a->Hq * a->kv.dh) return fail(RPO_EINVAL, "%s: q_stride shorter than a row", who);
+    if (!(scale > 0.f) || isinf(scale)) return fail(RPO_EINVAL, "%s: scale must be finite and > 0", who);
+    if ((ws == nullptr) != (ws_bytes == 0)) return fail(RPO_EINVAL, "%s: ws_dev / ws_bytes mismatch", who);
+    if ((uintptr_t)ws % 16) return fail(RPO_EINVAL, "%s: ws_dev must be 16-byte aligned", who);
+    if ((uintptr_t)q % dtype_size(a->kv.dtype)) return fail(RPO_EINVAL, "%s: q_dev is not aligned to its elements", who);
+    a->q = q;
+    a->q_stride = q_stride;
+    a->cu = cu;
+    a->scale = scale;
+    a->ws = ws;
+    a->ws_bytes = ws_bytes;
+    return RPO_OK;
+}
+
+}  // namespace
+
+extern "C" int rpo_batch_kv(const rpo_batch* b, int32_t layer, rpo_paged_kv* out) {
+    if (!b || !out) return fail(RPO_EINVAL, "rpo_batch_kv: NULL argument");
+    const rpo_model_desc& d = b->m->d;
+    if (layer < 0 || layer >= d.n_layers) return fail(RPO_EINVAL, "rpo_batch_kv: layer out of range");
+    if (b->state != kForked) return fail(RPO_ESTATE, "rpo_batch_kv: call rpo_kv_fork first");
+    out->pool_dev = (char*)b->kv + b->geom.layer_stride() * layer * dtype_size(d.dtype);
+    out->table_dev = b->at<int32_t>(b->L.tables) + b->rollout_table_off(0);
+    out->len_dev = nullptr;
+    out->page_stride = b->geom.page_stride();
+    out->n_pages = (int32_t)b->geom.n_pages;
+    out->n_seqs = b->bd.B;
+    out->table_stride = b->bd.table_len;
+    out->page_tokens = b->bd.pt;
+    out->n_kv_heads = d.n_kv_heads;
+    out->head_dim = d.head_dim;
+    out->dtype = d.dtype;
+    return RPO_OK;
+}
+
+extern "C" int rpo_kv_append(const rpo_paged_kv* kv, const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                             const int32_t* cu_rows_dev, int32_t n_rows, int32_t max_new, void* stream) {
+    PagedAppendArgs a;
+    int rc = paged_kv("rpo_kv_append", kv, true, &a.kv);
+    if (rc == RPO_OK) rc = rows_args("rpo_kv_append", cu_rows_dev, n_rows, max_new);
+    if (rc != RPO_OK) return rc;
+    if (n_rows > 0 && (!k_dev || !v_dev)) return fail(RPO_EINVAL, "rpo_kv_append: NULL argument");
+    const int64_t width = (int64_t)a.kv.Hkv * a.kv.dh;
+    if (k_stride < width || v_stride < width) return fail(RPO_EINVAL, "rpo_kv_append: k_stride / v_stride shorter than a row");
+    if (((uintptr_t)k_dev | (uintptr_t)v_dev) % dtype_size(a.kv.dtype))
+        return fail(RPO_EINVAL, "rpo_kv_append: rows are not aligned to their elements");
+    a.k = k_dev;
+    a.v = v_dev;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.cu = cu_rows_dev;
+    a.n_rows = n_rows;
+    a.max_new = max_new;
+    HIP_TRY(launch_paged_append(a, (hipStream_t)stream));
+    return RPO_OK;
+}
+
+extern "C" size_t rpo_attn_paged_ws_bytes(const rpo_paged_kv* kv, int32_t n_rows, int32_t max_new, int32_t max_len,
+                                          int32_t n_q_heads, int32_t window, int32_t n_sinks) {
+    PagedAttnArgs a;
+    if (attn_args("rpo_attn_paged_ws_bytes", kv, n_rows, max_new, max_len, n_q_heads, window, n_sinks, &a) != RPO_OK) return 0;
+    return paged_attn_ws_bytes(a);
+}
+
+extern "C" int rpo_attn_paged(const rpo_paged_kv* kv, const void* q_dev, int64_t q_stride, const int32_t* cu_rows_dev,
+                              int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads, float scale,
+                              int32_t window, int32_t n_sinks, void* out_dev, int64_t out_stride, float* lse_out_dev,
+                              void* ws_dev, size_t ws_bytes, void* stream) {
+    PagedAttnArgs a;
+    int rc = attn_args("rpo_attn_paged", kv, n_rows, max_new, max_len, n_q_heads, window, n_sinks, &a);
+    if (rc == RPO_OK) rc = attn_pointers("rpo_attn_paged", &a, q_dev, q_stride, cu_rows_dev, scale, ws_dev, ws_bytes);
+    if (rc != RPO_OK) return rc;
+    if (n_rows > 0 && !out_dev) return fail(RPO_EINVAL, "rpo_attn_paged: NULL argument");
+    if (out_stride < (int64_t)n_q_heads * a.kv.dh) return fail(RPO_EINVAL, "rpo_attn_paged: out_stride shorter than a row");
+    if ((uintptr_t)out_dev % dtype_size(a.kv.dtype)) return fail(RPO_EINVAL, "rpo_attn_paged: out_dev is not aligned to its elements");
+    const size_t need = ws_dev ? paged_attn_ws_bytes(a) : 0;
+    if (ws_bytes < need) return fail(RPO_ENOMEM, "rpo_attn_paged: workspace: %zu bytes given, %zu needed", ws_bytes, need);
+    a.out = out_dev;
+    a.out_stride = out_stride;
+    a.lse = lse_out_dev;
+    HIP_TRY(launch_paged_attn(a, (hipStream_t)stream));
+    return RPO_OK;
+}
+
+extern "C" size_t rpo_kv_score_ws_bytes(const rpo_paged_kv* kv, int32_t n_rows, int32_t max_new, int32_t max_len,
+                                        int32_t n_q_heads, int32_t window, int32_t n_sinks) {
+    PagedScoreArgs a;
+    if (attn_args("rpo_kv_score_ws_bytes", kv, n_rows, max_new, max_len, n_q_heads, window, n_sinks, &a.at) != RPO_OK) return 0;
+    return paged_score_ws_bytes(a);
+}
+
+extern "C" int rpo_kv_score(const rpo_paged_kv* kv, const void* q_dev, int64_t q_stride, const int32_t* cu_rows_dev,
+                            int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads, float scale, int32_t window,
+                            int32_t n_sinks, const float* lse_dev, const float* score_in_dev, float* score_out_dev,
+                            int64_t score_stride, void* ws_dev, size_t ws_bytes, void* stream) {
+    PagedScoreArgs a;
+    int rc = attn_args("rpo_kv_score", kv, n_rows, max_new, max_len, n_q_heads, window, n_sinks, &a.at);
+    if (rc == RPO_OK) rc = attn_pointers("rpo_kv_score", &a.at, q_dev, q_stride, cu_rows_dev, scale, ws_dev, ws_bytes);
+    if (rc != RPO_OK) return rc;
+    if ((n_rows > 0 && !lse_dev) || !score_out_dev) return fail(RPO_EINVAL, "rpo_kv_score: NULL argument");
+    if (score_stride < 1) return fail(RPO_EINVAL, "rpo_kv_score: score_stride must be >= 1");
+    const size_t need = ws_dev ? paged_score_ws_bytes(a) : 0;
+    if (ws_bytes < need) return fail(RPO_ENOMEM, "rpo_kv_score: workspace: %zu bytes given, %zu needed", ws_bytes, need);
+    a.lse_in = lse_dev;
+    a.score_in = score_in_dev;
+    a.score_out = score_out_dev;
+    a.score_stride = score_stride;
+    HIP_TRY(launch_paged_score(a, (hipStream_t)stream));
+    return RPO_OK;
+}
+
+extern "C" int rpo_kv_evict(const rpo_paged_kv* src, const float* score_dev, int64_t score_stride, int32_t budget,
+                            int32_t n_sinks, int32_t n_recent, const rpo_paged_kv* dst, int32_t* len_out_dev,
+                            float* score_out_dev, int64_t score_out_stride, int32_t* kept_out_dev, void* stream) {
+    PagedEvictArgs a;
+    int rc = paged_kv("rpo_kv_evict", src, true, &a.src);
+    if (rc == RPO_OK) rc = paged_kv("rpo_kv_evict", dst, false, &a.dst);
+    if (rc != RPO_OK) return rc;
+    if (!score_dev || !len_out_dev || !kept_out_dev) return fail(RPO_EINVAL, "rpo_kv_evict: NULL argument");
+    if (a.src.n_seqs != a.dst.n_seqs || a.src.Hkv != a.dst.Hkv || a.src.dh != a.dst.dh || a.src.dtype != a.dst.dtype)
+        return fail(RPO_EINVAL, "rpo_kv_evict: src and dst differ in n_seqs, n_kv_heads, head_dim or dtype");
+    if (n_sinks < 0 || n_recent < 0 || budget < 1 || (int64_t)n_sinks + n_recent > budget)
+        return fail(RPO_EINVAL, "rpo_kv_evict: need budget >= 1 and >= n_sinks + n_recent, neither below 0");
+    if (budget > ((int64_t)a.dst.table_stride << a.dst.shift))
+        return fail(RPO_EINVAL, "rpo_kv_evict: dst's table does not hold the budget");
+    if (score_stride < 1 || (score_out_dev && score_out_stride < budget))
+        return fail(RPO_EINVAL, "rpo_kv_evict: need score_stride >= 1 and score_out_stride >= budget");
+    if (score_out_dev == score_dev) return fail(RPO_EINVAL, "rpo_kv_evict: score_out_dev must not be score_dev");
+    if (a.src.table == a.dst.table && a.src.pool == a.dst.pool)
+        return fail(RPO_EINVAL, "rpo_kv_evict: dst's pages must not be src's");
+    a.score = score_dev;
+    a.score_stride = score_stride;
+    a.budget = budget;
+    a.sinks = n_sinks;
+    a.recent = n_recent;
+    a.len_out = len_out_dev;
+    a.score_out = score_out_dev;
+    a.score_out_stride = score_out_stride;
+    a.kept = kept_out_dev;
+    HIP_TRY(launch_paged_evict(a, (hipStream_t)stream));
+    return RPO_OK;
+}
