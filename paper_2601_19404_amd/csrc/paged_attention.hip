@@ -5,8 +5,18 @@
 //   out = sum_j p_j v_j,  p_j = exp(scale q.k_j - lse),  lse = ln sum_j exp(scale q.k_j)
 // A row that sees nothing leaves zeros and an lse of -infinity.
 //
-//  * attn_rows_kernel: one wave per (row, query head), any head_dim.
-//  * score_rows_kernel: one workgroup per 32 tokens of a KV head, any head_dim.
+//  * attn_tile_kernel: chunks, head_dim 32, 64 or 128, bf16 or fp32.  Four waves of 16 or 32 query columns (row x head of a KV
+//    head) each; keys and values go through LDS in tiles of 64 (32) tokens, straight from the pages, double buffered.
+//  * attn_few_kernel: up to 16 query columns per KV head (single tokens).  Every wave streams tokens of its own from the pages
+//    into the operand registers of the matrix instructions; the four waves' results are joined in LDS.
+//  * attn_join_kernel: joins the pieces of tokens that were split over workgroups.
+//  * score_tile_kernel, score_few_kernel: the weights summed over the query columns, keys in registers.
+//  * attn_rows_kernel, score_rows_kernel: any head_dim, one wave per (row, head), one workgroup per 32 tokens.
+//
+// Both element types go through the same code: a fragment is 16 bytes of a row per lane, which one 16x16x32 bf16 or four
+// 16x16x4 fp32 instructions multiply.  Scores are computed transposed, S^T = K Q^T, so that a lane holds scores of one query
+// column and its maximum and sum need two lane swaps; and the rows of K are dealt to the instruction such that the weights a
+// lane ends with are eight (four) consecutive tokens, which is how a page keeps the values: they are read as they lie.
 #include "kernels.hpp"
 
 namespace rpo {
@@ -16,6 +26,533 @@ namespace {
 // Whether a row at slot t sees slot j.
 __device__ inline bool sees(int t, int j, int window, int sinks) {
     return j <= t && (window == 0 || j < sinks || t - j < window);
+}
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <typename T>
+struct Mat;
+template <>
+struct Mat<bf16> {
+    static constexpr int kGroup = 32;  // tokens of one product of weights and values
+    // token of row c (0..15) of 16-token block mb: blocks 2 k and 2 k + 1 share 32 tokens, such that lane group g's rows
+    // 4 g .. 4 g + 3 of both are the tokens 8 g .. 8 g + 7
+    static __host__ __device__ constexpr int token(int mb, int c) { return 32 * (mb >> 1) + 8 * (c >> 2) + 4 * (mb & 1) + (c & 3); }
+    static __device__ constexpr int row_c(int r) { return 4 * ((r >> 3) & 3) + (r & 3); }  // the c of a token
+    static __device__ inline f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    }
+    // weights of 32 tokens as an operand: rounded to bf16 once
+    static __device__ inline u32x4_t weights(const f32x4_t* s) {
+        bf16x8_t p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = (__bf16)s[0][i], p[4 + i] = (__bf16)s[1][i];
+        return __builtin_bit_cast(u32x4_t, p);
+    }
+    // 16-byte unit of a values tile [octets][channels][8] that holds lane group g's tokens of group kk
+    static __device__ inline int unit(int kk, int g, int dh, int ch) { return (4 * kk + g) * dh + ch; }
+};
+template <>
+struct Mat<float> {
+    static constexpr int kGroup = 16;
+    static __host__ __device__ constexpr int token(int mb, int c) { return 16 * mb + c; }
+    static __device__ constexpr int row_c(int r) { return r & 15; }
+    static __device__ inline f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+        return c;
+    }
+    static __device__ inline u32x4_t weights(const f32x4_t* s) { return __builtin_bit_cast(u32x4_t, s[0]); }
+    static __device__ inline int unit(int kk, int g, int dh, int ch) { return ((2 * kk + (g >> 1)) * dh + ch) * 2 + (g & 1); }
+};
+
+// 16-byte pieces of a row, and where piece p of a row lies in LDS: permuted so that the 16 rows that a fragment reads at the
+// same piece fall on different banks (the LDS serves lanes 0-3, 12-15, 20-23 and 24-27 together)
+template <typename T, int DH>
+struct Row {
+    static constexpr int kBytes = DH * (int)sizeof(T), kPieces = kBytes / 16, kFrags = kPieces / 4;
+    static constexpr int kElems = 16 / (int)sizeof(T);  // elements of a piece
+    static __device__ inline int turn(int c) { return kPieces >= 16 ? c : kPieces == 8 ? c >> 1 : (4 - (c >> 2)) & 3; }
+};
+
+// in every lane the maximum (sum) over the four lanes that share l % 16
+template <typename F>
+__device__ inline float over_lane_groups(float v, F f) {
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+    u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_over_lane_groups(float v) {
+    return over_lane_groups(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ inline float sum_over_lane_groups(float v) {
+    return over_lane_groups(v, [](float a, float b) { return a + b; });
+}
+__device__ inline int wave_min_int(int v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ inline int wave_max_int(int v) { return -wave_min_int(-v); }
+// the same address in every lane, in scalar registers
+template <typename T>
+__device__ inline const T* uniform(const T* p) {
+    const uint64_t u = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+    return (const T*)(uintptr_t)((uint64_t)hi << 32 | lo);
+}
+
+// The slots that a set of rows sees any of, in steps of `step` tokens: [0, sink) and then [lo, hi), cut into pieces.
+struct Span {
+    int hi, lo, sinks;   // slots: seen if < hi and (< sinks or >= lo)
+    int sink_steps, lo_step, n;
+    __device__ Span(int t_first, int t_last, int window, int sinks_, int step) {
+        hi = max(t_last + 1, 0);
+        lo = window ? max(0, t_first - window + 1) : 0;
+        sinks = window ? min(sinks_, hi) : 0;
+        lo_step = lo / step;
+        sink_steps = min((sinks + step - 1) / step, lo_step);
+        n = sink_steps + max(0, (hi + step - 1) / step - lo_step);
+    }
+    __device__ int step_at(int i) const { return i < sink_steps ? i : lo_step + i - sink_steps; }
+    __device__ bool any(int j) const { return j < hi && (j < sinks || j >= lo); }
+};
+
+// ---------------------------------------------------------------------------
+// chunks
+// ---------------------------------------------------------------------------
+struct TileGeom {
+    int combos;   // n_seqs * Hkv
+    int n_split;  // pieces that the tokens are cut into
+    float* part;  // n_split > 1: [row, head, piece][DH] sums, then [row, head, piece][2] maximum (log2 domain) and sum
+};
+
+template <typename T, int DH, int NC>
+__global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, TileGeom geo) {
+    using R = Row<T, DH>;
+    using M = Mat<T>;
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32;       // tokens of a tile
+    constexpr int MB = KT / 16, KG = KT / M::kGroup;
+    constexpr int kTileBytes = KT * R::kBytes, kChunks = kTileBytes / 1024 / 4;  // 1 KiB loads per wave and tile
+    constexpr int kTok = 1024 / R::kBytes;             // tokens (of keys or of values) of a 1 KiB load
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTileBytes];  // keys, keys, values, values
+    const PagedKv& kv = a.kv;
+    const int combo = blockIdx.x % geo.combos, rest = blockIdx.x / geo.combos;
+    const int split = rest % geo.n_split, kh = combo % kv.Hkv, s = combo / kv.Hkv;
+    const ChunkRows cr = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
+    const int hpk = a.Hq / kv.Hkv;
+    constexpr int kCols = 64 * NC;
+    const int n_cols = cr.n * hpk, n_qt = (n_cols + kCols - 1) / kCols;
+    const int qt = n_qt - 1 - rest / geo.n_split;      // the longest contexts first
+    if (qt < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+
+    // this lane's query columns
+    int limit[NC], from[NC];     // sees slots < limit that are >= from or sinks
+    int64_t out_at[NC];          // row * Hq + head, -1: a padding column
+    u32x4_t bq[NC][R::kFrags];
+    int lim_min = 0x7fffffff, lim_max = 0, from_min = 0x7fffffff, from_max = 0;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int col = qt * kCols + (wave * NC + c) * 16 + c16;
+        const bool real = col < n_cols;
+        const int i = real ? col / hpk : 0, hq = kh * hpk + (real ? col % hpk : 0);
+        const int t = cr.slot0 + i;
+        out_at[c] = real ? (int64_t)(cr.row0 + i) * a.Hq + hq : -1;
+        limit[c] = real ? t + 1 : 0x7fffffff;
+        from[c] = real && a.window ? max(0, t - a.window + 1) : 0;
+        if (real) {
+            lim_min = min(lim_min, t + 1), lim_max = max(lim_max, t + 1);
+            from_min = min(from_min, from[c]), from_max = max(from_max, from[c]);
+        }
+        const T* q = (const T*)a.q + (int64_t)(cr.row0 + i) * a.q_stride + (int64_t)hq * DH;
+#pragma unroll
+        for (int j = 0; j < R::kFrags; ++j) bq[c][j] = real ? *(const u32x4_t*)(q + (4 * j + g) * R::kElems) : u32x4_t{0, 0, 0, 0};
+    }
+    lim_min = wave_min_int(lim_min), lim_max = wave_max_int(lim_max);
+    from_min = wave_min_int(from_min), from_max = wave_max_int(from_max);
+
+    const int first_row = qt * kCols / hpk, last_row = (min(n_cols, (qt + 1) * kCols) - 1) / hpk;
+    const Span span(cr.slot0 + first_row, cr.slot0 + last_row, a.window, a.sinks, KT);
+    const int per = (span.n + geo.n_split - 1) / geo.n_split;
+    const int it0 = min(span.n, split * per), it1 = min(span.n, it0 + per);
+
+    f32x4_t ot[NC][DH / 16];
+    float m[NC], l[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) ot[c][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m[c] = -INFINITY;
+        l[c] = 0.f;
+    }
+
+    // element offset of the KV head's keys of 16 tokens, -1: they are not there
+    auto unit_at = [&](int slot) -> int64_t {
+        int page = -1;
+        if (slot < span.hi) page = __builtin_amdgcn_readfirstlane(kv.page(s, slot));
+        return page < 0 ? -1 : kv.k_at(page, kh) + (int64_t)(slot & ((1 << kv.shift) - 1)) * DH;
+    };
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const int64_t to_values = (int64_t)kv.Hkv * kv.block();
+    int key_off[kChunks];  // lane's byte offset of its piece from the first token of the wave's i-th load
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int at = (i * 4 + wave) * 1024 + lane * 16, r = at / R::kBytes, slot = at % R::kBytes / 16;
+        key_off[i] = (r % kTok) * R::kBytes + ((slot ^ (R::turn(M::row_c(r)) & (R::kPieces - 1))) << 4);
+    }
+    int64_t unit[MB];
+    auto units = [&](int it) {
+        const int tok0 = span.step_at(it) * KT;
+#pragma unroll
+        for (int u = 0; u < MB; ++u) unit[u] = unit_at(tok0 + 16 * u);
+    };
+    auto load_tile = [&](int buf) {  // the tile whose units are at hand
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int first = (i * 4 + wave) * kTok, u = first >> 4;
+            int64_t at = unit[0];
+#pragma unroll
+            for (int x = 1; x < MB; ++x) at = u == x ? unit[x] : at;
+            if (at < 0) continue;  // uniform; what LDS holds there is masked, its values are cleared
+            const T* k = uniform((const T*)kv.pool + at + (int64_t)(first & 15) * DH);
+            dma_load16_at<false>(k, key_off[i], lds0 + buf * kTileBytes + wave * 1024, i * 4096);
+            dma_load16_at<false>(k + to_values, lane * 16, lds0 + (2 + buf) * kTileBytes + wave * 1024, i * 4096);
+        }
+    };
+    const float scale_log2 = a.scale * kLog2e;
+    const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+
+    if (it0 < it1) {
+        units(it0);
+        load_tile(0);
+    }
+    for (int it = it0; it < it1; ++it) {
+        const int buf = (it - it0) & 1, tok0 = span.step_at(it) * KT;
+        int gone = 0;  // bit u: the 16 tokens of unit u are not there
+#pragma unroll
+        for (int u = 0; u < MB; ++u) gone |= (unit[u] < 0) << u;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // the tile is there, and nobody reads the other buffer any more
+        asm volatile("" ::: "memory");
+        if (it + 1 < it1) {
+            units(it + 1);
+            load_tile(buf ^ 1);
+        }
+        const unsigned char* ks = smem + buf * kTileBytes;
+        unsigned char* vs = smem + (2 + buf) * kTileBytes;
+        // values that no row here sees may be anything: 0 x NaN must not reach a sum
+        if (gone || tok0 + KT > span.hi || (tok0 < span.lo && tok0 + KT > span.sinks)) {
+            constexpr int kUnitTok = 16 / (int)sizeof(T) > 4 ? 8 : 4;  // tokens of a 16-byte unit
+            for (int x = tid; x < kTileBytes / 16; x += 256) {
+                const int o = x * 16 / (8 * R::kBytes) * 8 + (sizeof(T) == 4 ? (x & 1) * 4 : 0);
+                T* e = (T*)(vs + x * 16);
+#pragma unroll
+                for (int y = 0; y < kUnitTok; ++y)
+                    if (!span.any(tok0 + o + y) || (gone >> ((o + y) >> 4) & 1)) e[y] = T{};
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        }
+        // nothing in this tile for the wave's rows
+        if (tok0 >= lim_max || (tok0 >= span.sinks && tok0 + KT <= from_min)) continue;
+        f32x4_t sc[NC][MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int j = 0; j < R::kFrags; ++j) {
+                const u32x4_t k = *(const u32x4_t*)(ks + M::token(mb, c16) * R::kBytes +
+                                                    (((4 * j + g) ^ (R::turn(c16) & (R::kPieces - 1))) << 4));
+#pragma unroll
+                for (int c = 0; c < NC; ++c) sc[c][mb] = M::mma(k, bq[c][j], j == 0 ? zero4 : sc[c][mb]);
+            }
+        const bool need_mask = gone || tok0 + KT > lim_min || (tok0 < from_max && tok0 + KT > span.sinks);
+        u32x4_t p[NC][KG];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            float top = -INFINITY;
+            if (need_mask) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = M::token(mb, 4 * g + i), j = tok0 + r;
+                        const bool seen = j < limit[c] && (j >= from[c] || j < span.sinks) && !(gone >> (r >> 4) & 1);
+                        sc[c][mb][i] = seen ? sc[c][mb][i] : -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][mb][i]);
+            const float mnew = fmaxf(m[c], max_over_lane_groups(top));
+            const float ref = mnew == -INFINITY ? 0.f : mnew;
+            const float alpha = __builtin_amdgcn_exp2f((m[c] - ref) * scale_log2), nb = -ref * scale_log2;
+            float sum = 0.f;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][mb][i], scale_log2, nb));
+                    sc[c][mb][i] = w;
+                    sum += w;
+                }
+            l[c] = l[c] * alpha + sum;
+            m[c] = mnew;
+            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+                for (int i = 0; i < DH / 16; ++i) ot[c][i] *= alpha;
+            }
+#pragma unroll
+            for (int kk = 0; kk < KG; ++kk) p[c][kk] = M::weights(&sc[c][kk * (M::kGroup / 16)]);
+        }
+#pragma unroll
+        for (int kk = 0; kk < KG; ++kk)
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) {
+                const u32x4_t v = *(const u32x4_t*)(vs + (M::unit(kk, g, DH, 16 * i + c16) << 4));
+#pragma unroll
+                for (int c = 0; c < NC; ++c) ot[c][i] = M::mma(v, p[c][kk], ot[c][i]);
+            }
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const float total = sum_over_lane_groups(l[c]);
+        if (out_at[c] < 0) continue;
+        if (geo.n_split > 1) {
+            const int64_t piece = out_at[c] * geo.n_split + split;
+            float* ml = geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH + 2 * piece;
+            if (g == 0) ml[0] = m[c] * scale_log2, ml[1] = total;
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)(geo.part + piece * DH + 16 * i + 4 * g) = ot[c][i];
+            continue;
+        }
+        const float inv = total > 0.f ? 1.0f / total : 0.f;
+        const int64_t row = out_at[c] / a.Hq;
+        T* out = (T*)a.out + row * a.out_stride + (out_at[c] - row * a.Hq) * DH;
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[16 * i + 4 * g + e] = from_f32<T>(ot[c][i][e] * inv);
+        if (a.lse && g == 0) a.lse[out_at[c]] = total > 0.f ? m[c] * a.scale + logf(total) : -INFINITY;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// up to 16 query columns per KV head
+// ---------------------------------------------------------------------------
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileGeom geo) {
+    using R = Row<T, DH>;
+    using M = Mat<T>;
+    constexpr int KS = M::kGroup, MB = KS / 16;  // tokens of a step
+    __shared__ __attribute__((aligned(16))) float os[4][16][DH];
+    __shared__ float ms[4][16], ls[4][16];
+    const PagedKv& kv = a.kv;
+    const int combo = blockIdx.x % geo.combos, split = blockIdx.x / geo.combos;
+    const int kh = combo % kv.Hkv, s = combo / kv.Hkv, hpk = a.Hq / kv.Hkv;
+    const ChunkRows cr = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
+    const int n_cols = cr.n * hpk;  // <= 16
+    if (n_cols == 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const Span span(cr.slot0, cr.slot0 + cr.n - 1, a.window, a.sinks, KS);
+    const int per = (span.n + geo.n_split - 1) / geo.n_split;
+    const int it0 = min(span.n, split * per), it1 = min(span.n, it0 + per);
+
+    const bool real = c16 < n_cols;
+    const int i_row = real ? c16 / hpk : 0, hq = kh * hpk + (real ? c16 % hpk : 0), t = cr.slot0 + i_row;
+    const int limit = t + 1, from = a.window ? max(0, t - a.window + 1) : 0;
+    u32x4_t bq[R::kFrags];
+    {
+        const T* q = (const T*)a.q + (int64_t)(cr.row0 + i_row) * a.q_stride + (int64_t)hq * DH;
+#pragma unroll
+        for (int j = 0; j < R::kFrags; ++j) bq[j] = *(const u32x4_t*)(q + (4 * j + g) * R::kElems);
+    }
+    // a lane's share of a step: a fragment of each 16-token block's keys, a unit of every 16 channels' values.  bf16 has
+    // both 16-token units of the pages in play, the one of the lane's key rows and the one of its values' octet.
+    const int key_tok = M::token(0, c16), key_unit = key_tok >> 4, val_unit = sizeof(T) == 2 ? g >> 1 : 0;
+    const int mask = (1 << kv.shift) - 1;
+    const T* pool = (const T*)kv.pool;
+    const int64_t to_values = (int64_t)kv.Hkv * kv.block();
+    auto page_of = [&](int it, int u) {
+        const int slot = span.step_at(it) * KS + 16 * u;
+        return it < it1 && slot < span.hi ? kv.page(s, slot) : -1;
+    };
+    u32x4_t ak[2][MB][R::kFrags], av[2][DH / 16];
+    auto load = [&](int it, int pk, int pv, u32x4_t (&k)[MB][R::kFrags], u32x4_t (&v)[DH / 16]) {
+        const int tok0 = span.step_at(it) * KS;
+        // a page that is not there: page 0 is read in its place, and masked
+        const T* kp = pool + kv.k_at(max(pk, 0), kh) + (int64_t)((tok0 + key_tok) & mask) * DH + g * R::kElems;
+        const T* vp = pool + kv.k_at(max(pv, 0), kh) + to_values + (int64_t)((tok0 + 16 * val_unit) & mask) * DH;
+        // units of values from there: as M::unit counts them, less the 16-token units before
+        const int u0 = M::unit(0, g, DH, c16) - val_unit * 2 * DH;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int j = 0; j < R::kFrags; ++j)
+                k[mb][j] = *(const u32x4_t*)(kp + (M::token(mb, 0) - M::token(0, 0)) * DH + 4 * j * R::kElems);
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i)
+            v[i] = *(const u32x4_t*)(vp + (int64_t)(u0 + (sizeof(T) == 2 ? 16 : 32) * i) * R::kElems);
+    };
+    f32x4_t ot[DH / 16];
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) ot[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    const float scale_log2 = a.scale * kLog2e;
+    const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+    const int lim_min = wave_min_int(limit), from_max = wave_max_int(from);
+
+    auto step = [&](int it, int pk, int pv, u32x4_t (&k)[MB][R::kFrags], u32x4_t (&v)[DH / 16]) {
+        const int tok0 = span.step_at(it) * KS;
+        f32x4_t sc[MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int j = 0; j < R::kFrags; ++j) sc[mb] = M::mma(k[mb][j], bq[j], j == 0 ? zero4 : sc[mb]);
+        const uint64_t gone_k = __builtin_amdgcn_ballot_w64(pk < 0), gone_v = __builtin_amdgcn_ballot_w64(pv < 0);
+        if (gone_k || gone_v || tok0 + KS > lim_min || (tok0 < from_max && tok0 + KS > span.sinks)) {
+            // lanes 0-7 hold the first unit's page, 8-15 the second's (fp32: the only one's)
+            const int gone = (int)(gone_k & 1) | (int)(gone_k >> 8 & 1) << 1;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = M::token(mb, 4 * g + i), j = tok0 + r;
+                    const bool seen = j < limit && (j >= from || j < span.sinks) && !(gone >> (r >> 4) & 1);
+                    sc[mb][i] = seen ? sc[mb][i] : -INFINITY;
+                }
+            // values that no row sees may be anything
+            constexpr int kTok = sizeof(T) == 2 ? 8 : 4;
+            const int first = tok0 + kTok * g;
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) {
+                T e[kTok];
+                *(u32x4_t*)e = v[i];
+#pragma unroll
+                for (int y = 0; y < kTok; ++y)
+                    if (pv < 0 || !span.any(first + y)) e[y] = T{};
+                v[i] = *(const u32x4_t*)e;
+            }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[mb][i]);
+        const float mnew = fmaxf(m, max_over_lane_groups(top));
+        const float ref = mnew == -INFINITY ? 0.f : mnew;
+        const float alpha = __builtin_amdgcn_exp2f((m - ref) * scale_log2), nb = -ref * scale_log2;
+        float sum = 0.f;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2, nb));
+                sc[mb][i] = w;
+                sum += w;
+            }
+        l = l * alpha + sum;
+        m = mnew;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) ot[i] *= alpha;
+        }
+        const u32x4_t p = M::weights(sc);
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) ot[i] = M::mma(v[i], p, ot[i]);
+    };
+
+    // wave w takes steps it0 + w, it0 + w + 4, ...; the next step's fragments are on their way while one is multiplied
+    int it = it0 + wave;
+    int pk = page_of(it, key_unit), pv = page_of(it, val_unit);
+    int pk2 = page_of(it + 4, key_unit), pv2 = page_of(it + 4, val_unit);
+    if (it < it1) load(it, pk, pv, ak[0], av[0]);
+    while (it < it1) {
+        if (it + 4 < it1) load(it + 4, pk2, pv2, ak[1], av[1]);
+        int pk3 = page_of(it + 8, key_unit), pv3 = page_of(it + 8, val_unit);
+        step(it, pk, pv, ak[0], av[0]);
+        it += 4;
+        if (it >= it1) break;
+        if (it + 4 < it1) load(it + 4, pk3, pv3, ak[0], av[0]);
+        pk = page_of(it + 8, key_unit), pv = page_of(it + 8, val_unit);
+        step(it, pk2, pv2, ak[1], av[1]);
+        pk2 = pk, pv2 = pv;
+        pk = pk3, pv = pv3;
+        it += 4;
+    }
+    // join the four waves
+    const float wave_l = sum_over_lane_groups(l);
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)&os[wave][c16][16 * i + 4 * g] = ot[i];
+    if (g == 0) ms[wave][c16] = m * scale_log2, ls[wave][c16] = wave_l;
+    __syncthreads();
+    for (int x = tid; x < n_cols * (DH / 4); x += 256) {
+        const int c = x / (DH / 4), ch = x % (DH / 4) * 4;
+        float top = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, ms[w][c]);
+        f32x4_t o = zero4;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float wgt = ms[w][c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[w][c] - top);
+            total += wgt * ls[w][c];
+            o += wgt * *(const f32x4_t*)&os[w][c][ch];
+        }
+        const int i = c / hpk;
+        const int64_t row = cr.row0 + i, head = kh * hpk + c % hpk, at = row * a.Hq + head;
+        if (geo.n_split > 1) {
+            const int64_t piece = at * geo.n_split + split;
+            *(f32x4_t*)(geo.part + piece * DH + ch) = o;
+            float* ml = geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH + 2 * piece;
+            if (ch == 0) ml[0] = top, ml[1] = total;
+            continue;
+        }
+        const float inv = total > 0.f ? 1.0f / total : 0.f;
+        T* out = (T*)a.out + row * a.out_stride + head * DH + ch;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = from_f32<T>(o[e] * inv);
+        if (a.lse && ch == 0) a.lse[at] = total > 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
+    }
+}
+
+// One workgroup per (row, heads): the pieces of a row's heads by their maxima.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeom geo) {
+    const int s = blockIdx.y, n_split = geo.n_split;
+    const ChunkRows cr = chunk_rows(a.kv, a.cu, s, a.n_rows, a.max_new);
+    const int per_row = a.Hq * (DH / 4);
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int i = (int)(x / per_row);
+    if (i >= cr.n) return;
+    const int head = (int)(x % per_row) / (DH / 4), ch = (int)(x % (DH / 4)) * 4;
+    const int64_t row = cr.row0 + i, at = row * a.Hq + head, piece = at * n_split;
+    const float* ml = geo.part + (int64_t)a.n_rows * a.Hq * n_split * DH + 2 * piece;
+    const float* po = geo.part + piece * DH + ch;
+    float top = -INFINITY;
+    for (int p = 0; p < n_split; ++p) top = fmaxf(top, ml[2 * p]);
+    float total = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < n_split; ++p) {
+        if (ml[2 * p] == -INFINITY) continue;  // saw nothing
+        const float wgt = __builtin_amdgcn_exp2f(ml[2 * p] - top);
+        total += wgt * ml[2 * p + 1];
+        o += wgt * *(const f32x4_t*)(po + (int64_t)p * DH);
+    }
+    const float inv = total > 0.f ? 1.0f / total : 0.f;
+    T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH + ch;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = from_f32<T>(o[e] * inv);
+    if (a.lse && ch == 0) a.lse[at] = total > 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -123,13 +660,74 @@ __global__ __launch_bounds__(256) void score_rows_kernel(PagedScoreArgs b) {
     }
 }
 
+// Whether the matrix kernels take a call: fragments are 16 aligned bytes, offsets inside a tile of rows 32 bits.
+bool tiles_take(const PagedAttnArgs& a) {
+    const int es = (int)dtype_size(a.kv.dtype);
+    return a.path != 1 && (a.kv.dh == 32 || a.kv.dh == 64 || a.kv.dh == 128) && (uintptr_t)a.q % 16 == 0 && a.q_stride * es % 16 == 0;
+}
+bool few_take(const PagedAttnArgs& a) { return (int64_t)a.max_new * (a.Hq / a.kv.Hkv) <= 16; }
+
+// Slots that the rows of a chunk see at most.
+int most_seen(const PagedAttnArgs& a) {
+    const int64_t w = a.window ? (int64_t)a.window + a.max_new + a.sinks : a.max_len;
+    return (int)(w < a.max_len ? w : a.max_len);
+}
+
+// Pieces that the tokens of a sequence are cut into, so that a few hundred workgroups work; none shorter than eight steps of
+// the few-column kernel (two a wave) or two tiles.
+int attn_splits(const PagedAttnArgs& a) {
+    if (a.kv.n_seqs < 1 || a.max_new < 1 || a.max_len < 1 || !tiles_take(a)) return 1;
+    const int hpk = a.Hq / a.kv.Hkv, es = (int)dtype_size(a.kv.dtype);
+    const bool few = few_take(a);
+    const int64_t tiles = few ? 1 : ceil_div64((int64_t)a.max_new * hpk, (int64_t)a.max_new * hpk <= 64 ? 64 : 128);
+    const int64_t groups = (int64_t)a.kv.n_seqs * a.kv.Hkv * tiles;
+    const int step = few ? 8 * (es == 2 ? 32 : 16) : 2 * (es == 2 ? 64 : 32);
+    const int64_t want = ceil_div64(512, groups), cap = most_seen(a) / step > 0 ? most_seen(a) / step : 1;
+    const int64_t n = want < cap ? want : cap;
+    return (int)(n < 64 ? n : 64);
+}
+
+template <typename T, int DH>
+hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
+    TileGeom geo;
+    geo.combos = a.kv.n_seqs * a.kv.Hkv;
+    geo.n_split = a.ws ? attn_splits(a) : 1;
+    geo.part = (float*)a.ws;
+    const int hpk = a.Hq / a.kv.Hkv;
+    const int64_t cols = (int64_t)a.max_new * hpk;
+    const int64_t tiles = few_take(a) ? 1 : ceil_div64(cols, cols <= 64 ? 64 : 128);
+    const int64_t grid = tiles * geo.combos * geo.n_split;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    if (few_take(a))
+        attn_few_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(a, geo);
+    else if (cols <= 64)
+        attn_tile_kernel<T, DH, 1><<<(unsigned)grid, 256, 0, s>>>(a, geo);
+    else
+        attn_tile_kernel<T, DH, 2><<<(unsigned)grid, 256, 0, s>>>(a, geo);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || geo.n_split == 1) return e;
+    const int64_t per = ceil_div64((int64_t)a.max_new * a.Hq * (DH / 4), 256);
+    if (per > 0x7fffffff) return hipErrorInvalidValue;
+    attn_join_kernel<T, DH><<<dim3((unsigned)per, a.kv.n_seqs), 256, 0, s>>>(a, geo);
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t paged_attn_ws_bytes(const PagedAttnArgs&) { return 0; }
+size_t paged_attn_ws_bytes(const PagedAttnArgs& a) {
+    const int n = attn_splits(a);
+    return n == 1 ? 0 : (size_t)a.n_rows * a.Hq * n * (a.kv.dh + 2) * 4;
+}
 size_t paged_score_ws_bytes(const PagedScoreArgs&) { return 0; }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
     if (a.n_rows <= 0 || a.kv.n_seqs <= 0 || a.max_new <= 0) return hipSuccess;
+    if (tiles_take(a)) {
+        const bool f32 = a.kv.dtype == kF32;
+        if (a.kv.dh == 128) return f32 ? launch_tiles<float, 128>(a, s) : launch_tiles<bf16, 128>(a, s);
+        if (a.kv.dh == 64) return f32 ? launch_tiles<float, 64>(a, s) : launch_tiles<bf16, 64>(a, s);
+        return f32 ? launch_tiles<float, 32>(a, s) : launch_tiles<bf16, 32>(a, s);
+    }
     const dim3 grid(a.max_new, a.Hq, a.kv.n_seqs);
     if (a.kv.dtype == kF32)
         attn_rows_kernel<float><<<grid, 64, 0, s>>>(a);
