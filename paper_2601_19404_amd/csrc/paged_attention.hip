@@ -556,6 +556,242 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeo
 }
 
 // ---------------------------------------------------------------------------
+// scores: the weights of a token summed over the query columns.  Products the other way round, S = Q K^T, so that a lane
+// holds scores of one token and its sum stays in one register; the keys of a wave's tokens stay in registers throughout.
+// ---------------------------------------------------------------------------
+struct ScoreGeom {
+    int combos;
+    int n_split;  // pieces that the query columns are cut into
+    float* part;  // n_split > 1: [piece, sequence, KV head][max_len] sums
+};
+
+// 16-token blocks of a wave: 64 VGPRs of keys at 128 channels
+template <typename T>
+constexpr int kScoreBlocks = sizeof(T) == 2 ? 4 : 2;
+
+// A wave's keys as operands; bit mb of the result: block mb is not there.
+template <typename T, int DH>
+__device__ inline int load_keys(const PagedKv& kv, int s, int kh, int tok0, int len, u32x4_t (&k)[kScoreBlocks<T>][Row<T, DH>::kFrags]) {
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, mask = (1 << kv.shift) - 1;
+    int gone = 0;
+#pragma unroll
+    for (int mb = 0; mb < kScoreBlocks<T>; ++mb) {
+        const int slot = tok0 + 16 * mb;
+        const int page = slot < len ? __builtin_amdgcn_readfirstlane(kv.page(s, slot)) : -1;
+        const T* at = (const T*)kv.pool + kv.k_at(max(page, 0), kh) + (int64_t)((slot & mask) + c16) * DH + g * Row<T, DH>::kElems;
+        gone |= (page < 0) << mb;
+#pragma unroll
+        for (int j = 0; j < Row<T, DH>::kFrags; ++j)
+            k[mb][j] = page < 0 ? u32x4_t{0, 0, 0, 0} : *(const u32x4_t*)(at + 4 * j * Row<T, DH>::kElems);
+    }
+    return gone;
+}
+
+// Tokens' sums to where they go: lanes 0-15 hold the tokens tok0 + 16 mb + lane.
+template <int MB>
+__device__ inline void store_scores(const PagedScoreArgs& b, const ScoreGeom& geo, int combo, int split, int tok0, int len, int gone,
+                                    const float (&acc)[MB]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const float sum = (gone >> mb & 1) ? 0.f : sum_over_lane_groups(acc[mb]);
+        const int j = tok0 + 16 * mb + lane;
+        if (lane >= 16 || j >= len) continue;
+        if (geo.n_split > 1) {
+            geo.part[((int64_t)split * geo.combos + combo) * b.at.max_len + j] = sum;
+        } else {
+            const int64_t at = combo * b.score_stride + j;
+            b.score_out[at] = (b.score_in ? b.score_in[at] : 0.f) + sum;
+        }
+    }
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void score_few_kernel(PagedScoreArgs b, ScoreGeom geo) {
+    using R = Row<T, DH>;
+    using M = Mat<T>;
+    constexpr int MB = kScoreBlocks<T>;
+    const PagedAttnArgs& a = b.at;
+    const PagedKv& kv = a.kv;
+    const int combo = blockIdx.x % geo.combos, kh = combo % kv.Hkv, s = combo / kv.Hkv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    const int tok0 = (blockIdx.x / geo.combos * 4 + wave) * 16 * MB;
+    const int len = min((int)min((int64_t)kv.length(s), b.score_stride), a.max_len);
+    if (tok0 >= len) return;
+    const ChunkRows cr = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
+    const int hpk = a.Hq / kv.Hkv, n_cols = cr.n * hpk;
+    const Span span(cr.slot0, cr.slot0 + cr.n - 1, a.window, a.sinks, 16);
+    float acc[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) acc[mb] = 0.f;
+    const bool some = n_cols > 0 && tok0 < span.hi && (tok0 < span.sinks || tok0 + 16 * MB > span.lo);
+    if (!some && b.score_in == b.score_out) return;
+    int gone = 0;
+    if (some) {
+        u32x4_t k[MB][R::kFrags], q[R::kFrags];
+        gone = load_keys<T, DH>(kv, s, kh, tok0, len, k);
+        const int col = c16 < n_cols ? c16 : 0;
+        const T* qp = (const T*)a.q + (int64_t)(cr.row0 + col / hpk) * a.q_stride + (int64_t)(kh * hpk + col % hpk) * DH;
+#pragma unroll
+        for (int j = 0; j < R::kFrags; ++j) q[j] = *(const u32x4_t*)(qp + (4 * j + g) * R::kElems);
+        int t[4];
+        float shift[4];  // -lse in the log2 domain; what gives nothing is infinitely far down
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int x = 4 * g + i, y = x < n_cols ? x : 0;
+            const float lse = b.lse_in[(int64_t)(cr.row0 + y / hpk) * a.Hq + kh * hpk + y % hpk];
+            t[i] = cr.slot0 + y / hpk;
+            shift[i] = x < n_cols && lse != -INFINITY ? -lse * kLog2e : -INFINITY;
+        }
+        const float scale_log2 = a.scale * kLog2e;
+        const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            f32x4_t sc;
+#pragma unroll
+            for (int j = 0; j < R::kFrags; ++j) sc = M::mma(q[j], k[mb][j], j == 0 ? zero4 : sc);
+            const int tok = tok0 + 16 * mb + c16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], scale_log2, shift[i]));
+                acc[mb] += sees(t[i], tok, a.window, a.sinks) ? w : 0.f;
+            }
+        }
+    }
+    store_scores<MB>(b, geo, combo, 0, tok0, len, gone, acc);
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void score_tile_kernel(PagedScoreArgs b, ScoreGeom geo) {
+    using R = Row<T, DH>;
+    using M = Mat<T>;
+    constexpr int MB = kScoreBlocks<T>, QT = 64;      // query columns of a tile
+    constexpr int kTileBytes = QT * R::kBytes, kChunks = kTileBytes / 4096;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kTileBytes];
+    __shared__ __attribute__((aligned(16))) float shifts[2][QT];
+    __shared__ __attribute__((aligned(16))) int slots[2][QT];
+    const PagedAttnArgs& a = b.at;
+    const PagedKv& kv = a.kv;
+    const int combo = blockIdx.x % geo.combos, rest = blockIdx.x / geo.combos, split = rest % geo.n_split;
+    const int kh = combo % kv.Hkv, s = combo / kv.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g = lane >> 4;
+    const int wg0 = rest / geo.n_split * 64 * MB, tok0 = wg0 + wave * 16 * MB, tok1 = tok0 + 16 * MB;  // first blocks: most rows
+    const int len = min((int)min((int64_t)kv.length(s), b.score_stride), a.max_len);
+    if (wg0 >= len) return;
+    const ChunkRows cr = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
+    const int hpk = a.Hq / kv.Hkv;
+    // columns whose rows see any of the workgroup's tokens
+    const int first = min(cr.n, max(0, wg0 - cr.slot0));
+    const int64_t past = a.window && wg0 >= a.sinks ? (int64_t)wg0 + 64 * MB - 1 + a.window - cr.slot0 : cr.n;
+    const int last = (int)min((int64_t)cr.n, max(past, (int64_t)first));
+    const int tile0 = first * hpk / QT, n_tiles = first < last ? (last * hpk + QT - 1) / QT - tile0 : 0;
+    const int per = (n_tiles + geo.n_split - 1) / geo.n_split;
+    const int it0 = tile0 + min(n_tiles, split * per), it1 = min(tile0 + n_tiles, it0 + per);
+
+    u32x4_t k[MB][R::kFrags];
+    const int gone = load_keys<T, DH>(kv, s, kh, tok0, len, k);
+    float acc[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) acc[mb] = 0.f;
+
+    // a lane's column in the wave's i-th load: row and head, moved on by QT columns from tile to tile
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const int row_step = QT / hpk, head_step = QT % hpk;
+    int ci[kChunks], ch[kChunks], piece[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int at = (i * 4 + wave) * 1024 + lane * 16, c = at / R::kBytes, p = at % R::kBytes / 16;
+        ci[i] = (it0 * QT + c) / hpk;
+        ch[i] = (it0 * QT + c) % hpk;
+        piece[i] = (p ^ (R::turn(c & 15) & (R::kPieces - 1))) << 4;
+    }
+    int si = (it0 * QT + lane) / hpk, sh = (it0 * QT + lane) % hpk;  // wave 0: the column whose lse it fetches
+    float lse_next = 0.f;
+    int slot_next = 0;
+    auto load_tile = [&](int it, int buf) {
+        const int base = min(it * QT / hpk, cr.n - 1);
+        const T* q = uniform((const T*)a.q + (int64_t)(cr.row0 + base) * a.q_stride + (int64_t)kh * hpk * DH);
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int x = min(ci[i], cr.n - 1);  // columns behind the last row: any that exist, they give nothing
+            const uint32_t off = (uint32_t)((x - base) * (int)a.q_stride + ch[i] * DH) * (uint32_t)sizeof(T) + piece[i];
+            dma_load16_at<false>(q, off, lds0 + buf * kTileBytes + wave * 1024, i * 4096);
+            ci[i] += row_step, ch[i] += head_step;
+            if (ch[i] >= hpk) ch[i] -= hpk, ++ci[i];
+        }
+        if (wave == 0) {
+            const int x = min(si, cr.n - 1);
+            const float lse = b.lse_in[(int64_t)(cr.row0 + x) * a.Hq + kh * hpk + sh];
+            lse_next = si < cr.n && lse != -INFINITY ? -lse * kLog2e : -INFINITY;
+            slot_next = cr.slot0 + x;
+            si += row_step, sh += head_step;
+            if (sh >= hpk) sh -= hpk, ++si;
+        }
+    };
+    const float scale_log2 = a.scale * kLog2e;
+    const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+    if (it0 < it1) {
+        load_tile(it0, 0);
+        if (wave == 0) shifts[0][lane] = lse_next, slots[0][lane] = slot_next;
+    }
+    for (int it = it0; it < it1; ++it) {
+        const int buf = (it - it0) & 1;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // the tile is there, and nobody reads the other buffer any more
+        asm volatile("" ::: "memory");
+        const bool more = it + 1 < it1;
+        if (more) load_tile(it + 1, buf ^ 1);
+        const int t_min = cr.slot0 + it * QT / hpk, t_max = cr.slot0 + min(cr.n - 1, (it * QT + QT - 1) / hpk);
+        // rows of this tile that see any of the wave's tokens, and whether all see all
+        const bool some = t_max >= tok0 && (!a.window || t_min - (tok1 - 1) < a.window || tok0 < a.sinks) && tok0 < len;
+        const bool all = t_min >= tok1 - 1 && (!a.window || t_max - tok0 < a.window || tok1 <= a.sinks);
+        if (some) {
+#pragma unroll
+            for (int cg = 0; cg < QT / 16; ++cg) {
+                u32x4_t q[R::kFrags];
+#pragma unroll
+                for (int j = 0; j < R::kFrags; ++j)
+                    q[j] = *(const u32x4_t*)(smem + buf * kTileBytes + (cg * 16 + c16) * R::kBytes +
+                                             (((4 * j + g) ^ (R::turn(c16) & (R::kPieces - 1))) << 4));
+                const f32x4_t shift = *(const f32x4_t*)&shifts[buf][cg * 16 + 4 * g];
+                f32x4_t sc[MB];
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int j = 0; j < R::kFrags; ++j) sc[mb] = M::mma(q[j], k[mb][j], j == 0 ? zero4 : sc[mb]);
+                if (all) {
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[mb] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2, shift[i]));
+                } else {
+                    int t[4];
+                    *(u32x4_t*)t = *(const u32x4_t*)&slots[buf][cg * 16 + 4 * g];
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2, shift[i]));
+                            acc[mb] += sees(t[i], tok0 + 16 * mb + c16, a.window, a.sinks) ? w : 0.f;
+                        }
+                }
+            }
+        }
+        if (more && wave == 0) shifts[buf ^ 1][lane] = lse_next, slots[buf ^ 1][lane] = slot_next;
+    }
+    store_scores<MB>(b, geo, combo, split, tok0, len, gone, acc);
+}
+
+__global__ __launch_bounds__(256) void score_join_kernel(PagedScoreArgs b, ScoreGeom geo) {
+    const int combo = blockIdx.y, s = combo / b.at.kv.Hkv, j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= min(min((int64_t)b.at.kv.length(s), b.score_stride), (int64_t)b.at.max_len)) return;
+    float sum = 0.f;
+    for (int p = 0; p < geo.n_split; ++p) sum += geo.part[((int64_t)p * geo.combos + combo) * b.at.max_len + j];
+    const int64_t at = combo * b.score_stride + j;
+    b.score_out[at] = (b.score_in ? b.score_in[at] : 0.f) + sum;
+}
+
+// ---------------------------------------------------------------------------
 // any head_dim: a wave streams 64 tokens at a time, a lane to a token for the scores, a lane to a channel for the values
 // ---------------------------------------------------------------------------
 template <typename T>
@@ -625,7 +861,7 @@ __global__ __launch_bounds__(256) void score_rows_kernel(PagedScoreArgs b) {
     const PagedAttnArgs& a = b.at;
     const PagedKv& kv = a.kv;
     const int kh = blockIdx.y, s = blockIdx.z, j0 = blockIdx.x * 32, tid = threadIdx.x;
-    const int len = (int)min((int64_t)kv.length(s), b.score_stride);
+    const int len = min((int)min((int64_t)kv.length(s), b.score_stride), a.max_len);
     if (j0 >= len) return;
     const int dh = kv.dh, hpk = a.Hq / kv.Hkv, mask = (1 << kv.shift) - 1;
     const ChunkRows c = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
@@ -712,13 +948,52 @@ hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Offsets of a tile's query rows from its first one are 32 bits.
+bool score_tiles_take(const PagedScoreArgs& b) {
+    return tiles_take(b.at) && b.at.q_stride < ((int64_t)1 << 30) / 66 / (int)dtype_size(b.at.kv.dtype);
+}
+
+// Pieces that the query columns are cut into: about four workgroups per CU, none of fewer than eight tiles.
+int score_splits(const PagedScoreArgs& b) {
+    const PagedAttnArgs& a = b.at;
+    if (a.kv.n_seqs < 1 || a.max_new < 1 || a.max_len < 1 || !score_tiles_take(b) || few_take(a)) return 1;
+    const int64_t rows = a.window && a.window + (int64_t)256 < a.max_new ? a.window + 256 : a.max_new;
+    const int64_t tiles = ceil_div64(rows * (a.Hq / a.kv.Hkv), 64);
+    const int64_t groups = (int64_t)a.kv.n_seqs * a.kv.Hkv * ceil_div(a.max_len, a.kv.dtype == kF32 ? 128 : 256);
+    const int64_t want = ceil_div64(1024, groups), cap = tiles / 8 > 0 ? tiles / 8 : 1;
+    const int64_t n = want < cap ? want : cap;
+    return (int)(n < 16 ? n : 16);
+}
+
+template <typename T, int DH>
+hipError_t launch_score_tiles(const PagedScoreArgs& b, hipStream_t s) {
+    const PagedAttnArgs& a = b.at;
+    ScoreGeom geo;
+    geo.combos = a.kv.n_seqs * a.kv.Hkv;
+    geo.n_split = a.ws ? score_splits(b) : 1;
+    geo.part = (float*)a.ws;
+    const int64_t grid = (int64_t)ceil_div(a.max_len, 64 * kScoreBlocks<T>) * geo.combos * geo.n_split;
+    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    if (few_take(a))
+        score_few_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(b, geo);
+    else
+        score_tile_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(b, geo);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || geo.n_split == 1) return e;
+    score_join_kernel<<<dim3(ceil_div(a.max_len, 256), geo.combos), 256, 0, s>>>(b, geo);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t paged_attn_ws_bytes(const PagedAttnArgs& a) {
     const int n = attn_splits(a);
     return n == 1 ? 0 : (size_t)a.n_rows * a.Hq * n * (a.kv.dh + 2) * 4;
 }
-size_t paged_score_ws_bytes(const PagedScoreArgs&) { return 0; }
+size_t paged_score_ws_bytes(const PagedScoreArgs& b) {
+    const int n = score_splits(b);
+    return n == 1 ? 0 : (size_t)n * b.at.kv.n_seqs * b.at.kv.Hkv * b.at.max_len * 4;
+}
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
     if (a.n_rows <= 0 || a.kv.n_seqs <= 0 || a.max_new <= 0) return hipSuccess;
@@ -739,6 +1014,12 @@ hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
 hipError_t launch_paged_score(const PagedScoreArgs& b, hipStream_t s) {
     const PagedAttnArgs& a = b.at;
     if (a.kv.n_seqs <= 0 || a.max_len <= 0) return hipSuccess;
+    if (score_tiles_take(b)) {
+        const bool f32 = a.kv.dtype == kF32;
+        if (a.kv.dh == 128) return f32 ? launch_score_tiles<float, 128>(b, s) : launch_score_tiles<bf16, 128>(b, s);
+        if (a.kv.dh == 64) return f32 ? launch_score_tiles<float, 64>(b, s) : launch_score_tiles<bf16, 64>(b, s);
+        return f32 ? launch_score_tiles<float, 32>(b, s) : launch_score_tiles<bf16, 32>(b, s);
+    }
     const dim3 grid(ceil_div(a.max_len, 32), a.kv.Hkv, a.kv.n_seqs);
     if (a.kv.dtype == kF32)
         score_rows_kernel<float><<<grid, 256, 0, s>>>(b);
