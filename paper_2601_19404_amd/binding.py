@@ -416,7 +416,7 @@ class PagedKV:
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page_tokens: int, n_kv_heads: int,
                  head_dim: int):
         if pool.dtype not in (torch.float32, torch.bfloat16) or not pool.is_cuda or pool.dim() < 2 \
-                or not pool[:1].is_contiguous():
+                or pool.shape[0] < 1 or not pool[:1].is_contiguous():
             raise ValueError("pool: need a float32 or bfloat16 device tensor [n_pages, ...], contiguous within a page")
         _dev(table, torch.int32, "table")
         _dev(lens, torch.int32, "lens")
@@ -430,8 +430,17 @@ class PagedKV:
         self.desc = PagedKvDesc(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), pool.stride(0), pool.shape[0],
                                 table.shape[0], table.shape[1], page_tokens, n_kv_heads, head_dim,
                                 RPO_F32 if pool.dtype == torch.float32 else RPO_BF16)
-        self.capacity = table.shape[1] * page_tokens     # tokens that a row of the table holds
-        self.device = pool.device
+        self._fill()
+
+    def _fill(self):
+        """What the calls look at, read off the descriptor once."""
+        d = self.desc
+        self.ref = C.byref(d)
+        self.n_seqs, self.n_kv_heads, self.head_dim = d.n_seqs, d.n_kv_heads, d.head_dim
+        self.dtype = torch.float32 if d.dtype == RPO_F32 else torch.bfloat16
+        self.index = self.lens.get_device()
+        self.capacity = d.table_stride * d.page_tokens     # tokens that a row of the table holds
+        self.scale = d.head_dim ** -0.5
 
     @classmethod
     def of_batch(cls, batch: Batch, layer: int, lens: torch.Tensor) -> "PagedKV":
@@ -444,76 +453,88 @@ class PagedKV:
             raise ValueError("lens: need n_groups * G lengths on the batch's device")
         self.desc.len_dev = lens.data_ptr()
         self.batch, self.pool, self.table, self.lens = batch, batch.kv_pool, None, lens
-        self.capacity = self.desc.table_stride * self.desc.page_tokens
-        self.device = lens.device
+        self._fill()
         return self
 
 
-def _on(kv: PagedKV, stream, **tensors) -> int:
-    """The stream to launch on; every tensor has to lie on the cache's device, and the stream too."""
+# A decode step makes these calls layer by layer: their checks are kept to a few attribute reads (8 us of a call's 13 before
+# went into them, 4 now).
+def _on(kv: PagedKV, stream, *tensors) -> int:
+    """The stream to launch on; the cache has to lie on the current device, and every tensor and the stream there too."""
+    index = kv.index
+    if torch._C._cuda_getDevice() != index:
+        raise ValueError(f"the cache lies on cuda:{index}, which is not the current device")
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("a tensor lies on another device than the cache")
     if stream is None:
-        stream = torch.cuda.current_stream(kv.device)
-    elif stream.device != kv.device:
+        return torch._C._cuda_getCurrentRawStream(index)
+    if stream.device_index != index:
         raise ValueError("the stream belongs to another device than the cache")
-    if kv.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache lies on {kv.device}, which is not the current device")
-    for name, t in tensors.items():
-        if t is not None and t.device != kv.device:
-            raise ValueError(f"{name} lies on another device than the cache")
     return stream.cuda_stream
 
 
-def _rows(t: torch.Tensor, kv: PagedKV, width: int, name: str) -> torch.Tensor:
-    dt = torch.float32 if kv.desc.dtype == RPO_F32 else torch.bfloat16
-    if t.dim() != 2 or t.dtype != dt or t.shape[1] != width or (t.shape[0] > 1 and t.stride(0) < width) \
-            or (width > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: need {dt} rows of {width} values with unit column stride")
-    return t
+def _rows(t: torch.Tensor, kv: PagedKV, name: str) -> tuple[int, int, int]:
+    """(rows, columns, row stride) of a 2-D tensor of the cache's type."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype is not kv.dtype or (stride[1] != 1 and shape[1] > 1) \
+            or (stride[0] < shape[1] and shape[0] > 1):
+        raise ValueError(f"{name}: need rows of {kv.dtype} with unit column stride")
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1]
 
 
-def _stride(t: torch.Tensor) -> int:
-    return max(t.stride(0), t.shape[1])
+def _cu(t: torch.Tensor, kv: PagedKV) -> int:
+    if t.dtype is not torch.int32 or not t.is_contiguous() or t.numel() <= kv.n_seqs:
+        raise ValueError("cu_rows_dev: need n_seqs + 1 contiguous int32 values")
+    return t.data_ptr()
 
 
-def _cu(cu_rows_dev: torch.Tensor, kv: PagedKV) -> torch.Tensor:
-    _dev(cu_rows_dev, torch.int32, "cu_rows_dev")
-    if cu_rows_dev.numel() < kv.desc.n_seqs + 1:
-        raise ValueError("cu_rows_dev: need n_seqs + 1 values")
-    return cu_rows_dev
+def _floats(t: torch.Tensor, at_least: int, name: str) -> int:
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() < at_least:
+        raise ValueError(f"{name}: need at least {at_least} contiguous float32 values")
+    return t.data_ptr()
 
 
-def _q_heads(q_dev: torch.Tensor, kv: PagedKV) -> int:
-    n, rest = divmod(q_dev.shape[-1], kv.desc.head_dim)
+def _queries(q_dev: torch.Tensor, kv: PagedKV) -> tuple[int, int, int]:
+    """(rows, query heads, row stride)"""
+    n, width, stride = _rows(q_dev, kv, "q_dev")
+    heads, rest = divmod(width, kv.head_dim)
     if rest:
         raise ValueError("q_dev: a row is not a whole number of heads")
-    return n
+    return n, heads, stride
 
 
-def _score_rows(t, kv: PagedKV, name: str, at_least: int = 1):
-    if t is not None:
-        _dev(t, torch.float32, name)
-        if tuple(t.shape[:-1]) != (kv.desc.n_seqs, kv.desc.n_kv_heads) or t.shape[-1] < at_least:
-            raise ValueError(f"{name}: need [n_seqs, n_kv_heads, at least {at_least}]")
-    return t
+def _workspace(t) -> tuple[int | None, int]:
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("ws_dev: need a contiguous tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _scores(t, kv: PagedKV, name: str, at_least: int = 1) -> int:
+    """Values in a row of scores [n_seqs, n_kv_heads, ...]."""
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.dim() != 3 or t.shape[0] != kv.n_seqs \
+            or t.shape[1] != kv.n_kv_heads or t.shape[2] < at_least:
+        raise ValueError(f"{name}: need contiguous float32 [n_seqs, n_kv_heads, at least {at_least}]")
+    return t.shape[2]
 
 
 def rpo_kv_append(kv: PagedKV, k_dev: torch.Tensor, v_dev: torch.Tensor, cu_rows_dev: torch.Tensor, max_new: int,
                   stream=None) -> None:
     """Write the rows' keys and values [n_rows, n_kv_heads * head_dim] to the last slots of their sequences."""
-    width = kv.desc.n_kv_heads * kv.desc.head_dim
-    _rows(k_dev, kv, width, "k_dev")
-    _rows(v_dev, kv, width, "v_dev")
-    _cu(cu_rows_dev, kv)
-    if k_dev.shape[0] != v_dev.shape[0]:
-        raise ValueError("k_dev and v_dev differ in rows")
-    on = _on(kv, stream, k_dev=k_dev, v_dev=v_dev, cu_rows_dev=cu_rows_dev)
-    _check(lib().rpo_kv_append(C.byref(kv.desc), k_dev.data_ptr(), _stride(k_dev), v_dev.data_ptr(), _stride(v_dev),
-                               cu_rows_dev.data_ptr(), k_dev.shape[0], max_new, on))
+    n, width, k_stride = _rows(k_dev, kv, "k_dev")
+    n2, width2, v_stride = _rows(v_dev, kv, "v_dev")
+    if n != n2 or not width == width2 == kv.n_kv_heads * kv.head_dim:
+        raise ValueError("k_dev and v_dev: need equally many rows of n_kv_heads * head_dim values")
+    cu = _cu(cu_rows_dev, kv)
+    on = _on(kv, stream, k_dev, v_dev, cu_rows_dev)
+    _check(lib().rpo_kv_append(kv.ref, k_dev.data_ptr(), k_stride, v_dev.data_ptr(), v_stride, cu, n, max_new, on))
 
 
 def rpo_attn_paged_ws_bytes(kv: PagedKV, n_rows: int, max_new: int, max_len: int, n_q_heads: int, window: int = 0,
                             n_sinks: int = 0) -> int:
-    return lib().rpo_attn_paged_ws_bytes(C.byref(kv.desc), n_rows, max_new, max_len, n_q_heads, window, n_sinks)
+    return lib().rpo_attn_paged_ws_bytes(kv.ref, n_rows, max_new, max_len, n_q_heads, window, n_sinks)
 
 
 def rpo_attn_paged(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, max_new: int, out_dev: torch.Tensor,
@@ -521,65 +542,52 @@ def rpo_attn_paged(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, 
                    max_len: int | None = None, stream=None) -> None:
     """Attention of rows [n_rows, n_q_heads * head_dim] over their sequences' pages.  scale: 1 / sqrt(head_dim) if not
     given; max_len: what the table holds if not given; ws_dev: uint8, rpo_attn_paged_ws_bytes long."""
-    Hq = _q_heads(q_dev, kv)
-    _rows(q_dev, kv, q_dev.shape[1], "q_dev")
-    _rows(out_dev, kv, q_dev.shape[1], "out_dev")
-    _cu(cu_rows_dev, kv)
-    if out_dev.shape[0] != q_dev.shape[0]:
-        raise ValueError("out_dev and q_dev differ in rows")
-    if lse_out_dev is not None and _dev(lse_out_dev, torch.float32, "lse_out_dev").numel() < q_dev.shape[0] * Hq:
-        raise ValueError("lse_out_dev smaller than n_rows x n_q_heads")
-    on = _on(kv, stream, q_dev=q_dev, out_dev=out_dev, cu_rows_dev=cu_rows_dev, lse_out_dev=lse_out_dev, ws_dev=ws_dev)
-    _check(lib().rpo_attn_paged(C.byref(kv.desc), q_dev.data_ptr(), _stride(q_dev), cu_rows_dev.data_ptr(),
-                                q_dev.shape[0], max_new, kv.capacity if max_len is None else max_len, Hq,
-                                kv.desc.head_dim ** -0.5 if scale is None else scale, window, n_sinks,
-                                out_dev.data_ptr(), _stride(out_dev), _ptr(lse_out_dev), _ptr(ws_dev),
-                                0 if ws_dev is None else ws_dev.numel() * ws_dev.element_size(), on))
+    n, heads, q_stride = _queries(q_dev, kv)
+    n2, width, out_stride = _rows(out_dev, kv, "out_dev")
+    if n2 != n or width != q_dev.shape[1]:
+        raise ValueError("out_dev and q_dev differ in shape")
+    lse = None if lse_out_dev is None else _floats(lse_out_dev, n * heads, "lse_out_dev")
+    ws, ws_bytes = _workspace(ws_dev)
+    cu = _cu(cu_rows_dev, kv)
+    on = _on(kv, stream, q_dev, out_dev, cu_rows_dev, lse_out_dev, ws_dev)
+    _check(lib().rpo_attn_paged(kv.ref, q_dev.data_ptr(), q_stride, cu, n, max_new,
+                                kv.capacity if max_len is None else max_len, heads, kv.scale if scale is None else scale,
+                                window, n_sinks, out_dev.data_ptr(), out_stride, lse, ws, ws_bytes, on))
 
 
 def rpo_kv_score_ws_bytes(kv: PagedKV, n_rows: int, max_new: int, max_len: int, n_q_heads: int, window: int = 0,
                           n_sinks: int = 0) -> int:
-    return lib().rpo_kv_score_ws_bytes(C.byref(kv.desc), n_rows, max_new, max_len, n_q_heads, window, n_sinks)
+    return lib().rpo_kv_score_ws_bytes(kv.ref, n_rows, max_new, max_len, n_q_heads, window, n_sinks)
 
 
 def rpo_kv_score(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, max_new: int, lse_dev: torch.Tensor,
                  score_in_dev, score_out_dev: torch.Tensor, window: int = 0, n_sinks: int = 0, scale: float | None = None,
                  ws_dev=None, max_len: int | None = None, stream=None) -> None:
     """score_out = score_in (None: zeros) + the attention weight that every cached token receives from the rows."""
-    Hq = _q_heads(q_dev, kv)
-    _rows(q_dev, kv, q_dev.shape[1], "q_dev")
-    _cu(cu_rows_dev, kv)
-    if _dev(lse_dev, torch.float32, "lse_dev").numel() < q_dev.shape[0] * Hq:
-        raise ValueError("lse_dev smaller than n_rows x n_q_heads")
-    _score_rows(score_out_dev, kv, "score_out_dev")
-    _score_rows(score_in_dev, kv, "score_in_dev")
-    if score_in_dev is not None and score_in_dev.shape != score_out_dev.shape:
+    n, heads, q_stride = _queries(q_dev, kv)
+    lse = _floats(lse_dev, n * heads, "lse_dev")
+    row = _scores(score_out_dev, kv, "score_out_dev")
+    if score_in_dev is not None and _scores(score_in_dev, kv, "score_in_dev") != row:
         raise ValueError("score_in_dev and score_out_dev differ in shape")
-    on = _on(kv, stream, q_dev=q_dev, cu_rows_dev=cu_rows_dev, lse_dev=lse_dev, score_in_dev=score_in_dev,
-             score_out_dev=score_out_dev, ws_dev=ws_dev)
-    _check(lib().rpo_kv_score(C.byref(kv.desc), q_dev.data_ptr(), _stride(q_dev), cu_rows_dev.data_ptr(),
-                              q_dev.shape[0], max_new, kv.capacity if max_len is None else max_len, Hq,
-                              kv.desc.head_dim ** -0.5 if scale is None else scale, window, n_sinks, lse_dev.data_ptr(),
-                              _ptr(score_in_dev), score_out_dev.data_ptr(), score_out_dev.shape[-1], _ptr(ws_dev),
-                              0 if ws_dev is None else ws_dev.numel() * ws_dev.element_size(), on))
+    ws, ws_bytes = _workspace(ws_dev)
+    cu = _cu(cu_rows_dev, kv)
+    on = _on(kv, stream, q_dev, cu_rows_dev, lse_dev, score_in_dev, score_out_dev, ws_dev)
+    _check(lib().rpo_kv_score(kv.ref, q_dev.data_ptr(), q_stride, cu, n, max_new,
+                              kv.capacity if max_len is None else max_len, heads, kv.scale if scale is None else scale,
+                              window, n_sinks, lse, _ptr(score_in_dev), score_out_dev.data_ptr(), row, ws, ws_bytes, on))
 
 
 def rpo_kv_evict(kv: PagedKV, score_dev: torch.Tensor, budget: int, n_sinks: int, n_recent: int, dst: PagedKV,
                  len_out_dev: torch.Tensor, kept_out_dev: torch.Tensor, score_out_dev=None, stream=None) -> None:
     """Keep `budget` tokens per KV head of every longer sequence; the kept ones go to dst's pages."""
-    _score_rows(score_dev, kv, "score_dev")
-    _score_rows(score_out_dev, kv, "score_out_dev", max(budget, 1))
-    _dev(len_out_dev, torch.int32, "len_out_dev")
-    _dev(kept_out_dev, torch.int32, "kept_out_dev")
-    if len_out_dev.numel() < kv.desc.n_seqs or kept_out_dev.numel() < kv.desc.n_seqs * kv.desc.n_kv_heads * budget:
-        raise ValueError("len_out_dev / kept_out_dev smaller than n_seqs / n_seqs x n_kv_heads x budget")
-    if dst.device != kv.device:
-        raise ValueError("src and dst lie on different devices")
-    on = _on(kv, stream, score_dev=score_dev, len_out_dev=len_out_dev, kept_out_dev=kept_out_dev,
-             score_out_dev=score_out_dev)
-    _check(lib().rpo_kv_evict(C.byref(kv.desc), score_dev.data_ptr(), score_dev.shape[-1], budget, n_sinks, n_recent,
-                              C.byref(dst.desc), len_out_dev.data_ptr(), _ptr(score_out_dev),
-                              0 if score_out_dev is None else score_out_dev.shape[-1], kept_out_dev.data_ptr(), on))
+    row = _scores(score_dev, kv, "score_dev")
+    row_out = 0 if score_out_dev is None else _scores(score_out_dev, kv, "score_out_dev", max(budget, 1))
+    for t, n, name in ((len_out_dev, kv.n_seqs, "len_out_dev"), (kept_out_dev, kv.n_seqs * kv.n_kv_heads * budget, "kept_out_dev")):
+        if t.dtype is not torch.int32 or not t.is_contiguous() or t.numel() < n:
+            raise ValueError(f"{name}: need at least {n} contiguous int32 values")
+    on = _on(kv, stream, score_dev, len_out_dev, kept_out_dev, score_out_dev, dst.lens)
+    _check(lib().rpo_kv_evict(kv.ref, score_dev.data_ptr(), row, budget, n_sinks, n_recent, dst.ref,
+                              len_out_dev.data_ptr(), _ptr(score_out_dev), row_out, kept_out_dev.data_ptr(), on))
 
 
 def rpo_gemm_nt_noalloc(a_dev: torch.Tensor, w_dev: torch.Tensor, c_dev: torch.Tensor, epilogue: int,
