@@ -52,6 +52,12 @@ struct Mat<bf16> {
         for (int i = 0; i < 4; ++i) p[i] = (__bf16)s[0][i], p[4 + i] = (__bf16)s[1][i];
         return __builtin_bit_cast(u32x4_t, p);
     }
+    static __device__ inline u32x4_t times(u32x4_t p, float f) {
+        bf16x8_t x = __builtin_bit_cast(bf16x8_t, p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (__bf16)((float)x[i] * f);
+        return __builtin_bit_cast(u32x4_t, x);
+    }
     // 16-byte unit of a values tile [octets][channels][8] that holds lane group g's tokens of group kk
     static __device__ inline int unit(int kk, int g, int dh, int ch) { return (4 * kk + g) * dh + ch; }
 };
@@ -67,6 +73,7 @@ struct Mat<float> {
         return c;
     }
     static __device__ inline u32x4_t weights(const f32x4_t* s) { return __builtin_bit_cast(u32x4_t, s[0]); }
+    static __device__ inline u32x4_t times(u32x4_t p, float f) { return __builtin_bit_cast(u32x4_t, __builtin_bit_cast(f32x4_t, p) * f); }
     static __device__ inline int unit(int kk, int g, int dh, int ch) { return ((2 * kk + (g >> 1)) * dh + ch) * 2 + (g & 1); }
 };
 
@@ -133,12 +140,13 @@ struct TileGeom {
     float* part;  // n_split > 1: [row, head, piece][DH] sums, then [row, head, piece][2] maximum (log2 domain) and sum
 };
 
-template <typename T, int DH, int NC>
+template <typename T, int DH, int NC, bool WIDE>
 __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, TileGeom geo) {
     using R = Row<T, DH>;
     using M = Mat<T>;
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32;       // tokens of a tile
-    constexpr int MB = KT / 16, KG = KT / M::kGroup;
+    constexpr int KS = M::kGroup, KT = 2 * KS;         // tokens of a half tile (one step) and of a tile
+    constexpr int MB = KS / 16;                        // 16-token blocks of a step
+    constexpr int U = WIDE ? 1 : KT / 16;              // units of a tile that lie in one page: the tile, or 16 tokens
     constexpr int kTileBytes = KT * R::kBytes, kChunks = kTileBytes / 1024 / 4;  // 1 KiB loads per wave and tile
     constexpr int kTok = 1024 / R::kBytes;             // tokens (of keys or of values) of a 1 KiB load
     __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTileBytes];  // keys, keys, values, values
@@ -156,193 +164,314 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
 
     // this lane's query columns
     int limit[NC], from[NC];     // sees slots < limit that are >= from or sinks
-    int64_t out_at[NC];          // row * Hq + head, -1: a padding column
     u32x4_t bq[NC][R::kFrags];
-    int lim_min = 0x7fffffff, lim_max = 0, from_min = 0x7fffffff, from_max = 0;
+    int lim_min = 0x7fffffff, from_max = 0;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int col = qt * kCols + (wave * NC + c) * 16 + c16;
         const bool real = col < n_cols;
         const int i = real ? col / hpk : 0, hq = kh * hpk + (real ? col % hpk : 0);
         const int t = cr.slot0 + i;
-        out_at[c] = real ? (int64_t)(cr.row0 + i) * a.Hq + hq : -1;
         limit[c] = real ? t + 1 : 0x7fffffff;
         from[c] = real && a.window ? max(0, t - a.window + 1) : 0;
-        if (real) {
-            lim_min = min(lim_min, t + 1), lim_max = max(lim_max, t + 1);
-            from_min = min(from_min, from[c]), from_max = max(from_max, from[c]);
-        }
+        if (real) lim_min = min(lim_min, t + 1), from_max = max(from_max, from[c]);
         const T* q = (const T*)a.q + (int64_t)(cr.row0 + i) * a.q_stride + (int64_t)hq * DH;
 #pragma unroll
         for (int j = 0; j < R::kFrags; ++j) bq[c][j] = real ? *(const u32x4_t*)(q + (4 * j + g) * R::kElems) : u32x4_t{0, 0, 0, 0};
     }
-    lim_min = wave_min_int(lim_min), lim_max = wave_max_int(lim_max);
-    from_min = wave_min_int(from_min), from_max = wave_max_int(from_max);
+    lim_min = wave_min_int(lim_min), from_max = wave_max_int(from_max);
 
     const int first_row = qt * kCols / hpk, last_row = (min(n_cols, (qt + 1) * kCols) - 1) / hpk;
     const Span span(cr.slot0 + first_row, cr.slot0 + last_row, a.window, a.sinks, KT);
     const int per = (span.n + geo.n_split - 1) / geo.n_split;
-    const int it0 = min(span.n, split * per), it1 = min(span.n, it0 + per);
+    const int it0 = min(span.n, split * per), n = min(span.n - it0, per);  // this workgroup's tiles: it0 .. it0 + n - 1
 
     f32x4_t ot[NC][DH / 16];
-    float m[NC], l[NC];
+    // weights are 2^(scale_log2 score + minus_ref), minus_ref a whole number; it moves when a score passes bound (-infinity
+    // before the first one)
+    float minus_ref[NC], bound[NC], l[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
         for (int i = 0; i < DH / 16; ++i) ot[c][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        m[c] = -INFINITY;
+        minus_ref[c] = 0.f;
+        bound[c] = -INFINITY;
         l[c] = 0.f;
     }
 
-    // element offset of the KV head's keys of 16 tokens, -1: they are not there
-    auto unit_at = [&](int slot) -> int64_t {
-        int page = -1;
-        if (slot < span.hi) page = __builtin_amdgcn_readfirstlane(kv.page(s, slot));
-        return page < 0 ? -1 : kv.k_at(page, kh) + (int64_t)(slot & ((1 << kv.shift) - 1)) * DH;
-    };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    const int64_t to_values = (int64_t)kv.Hkv * kv.block();
-    int key_off[kChunks];  // lane's byte offset of its piece from the first token of the wave's i-th load
+    const int64_t to_values = (int64_t)kv.Hkv * kv.block() * (int64_t)sizeof(T);
+    // byte offset of a lane's piece of keys from the unit's first token (WIDE), or from the first token of the 1 KiB load
+    int key_off[kChunks];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
         const int at = (i * 4 + wave) * 1024 + lane * 16, r = at / R::kBytes, slot = at % R::kBytes / 16;
-        key_off[i] = (r % kTok) * R::kBytes + ((slot ^ (R::turn(M::row_c(r)) & (R::kPieces - 1))) << 4);
+        key_off[i] = (WIDE ? r : r % kTok) * R::kBytes + ((slot ^ (R::turn(M::row_c(r)) & (R::kPieces - 1))) << 4);
     }
-    int64_t unit[MB];
-    auto units = [&](int it) {
-        const int tok0 = span.step_at(it) * KT;
+    // page of every unit of a tile, -1: not there.  Left in a vector register for a tile's time before it is looked at.
+    const int32_t* const table = kv.table + (int64_t)s * kv.table_stride;
+    auto pages = [&](int x, int (&page)[U]) {
+        const int slot = span.step_at(it0 + x) * KT;
 #pragma unroll
-        for (int u = 0; u < MB; ++u) unit[u] = unit_at(tok0 + 16 * u);
-    };
-    auto load_tile = [&](int buf) {  // the tile whose units are at hand
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            const int first = (i * 4 + wave) * kTok, u = first >> 4;
-            int64_t at = unit[0];
-#pragma unroll
-            for (int x = 1; x < MB; ++x) at = u == x ? unit[x] : at;
-            if (at < 0) continue;  // uniform; what LDS holds there is masked, its values are cleared
-            const T* k = uniform((const T*)kv.pool + at + (int64_t)(first & 15) * DH);
-            dma_load16_at<false>(k, key_off[i], lds0 + buf * kTileBytes + wave * 1024, i * 4096);
-            dma_load16_at<false>(k + to_values, lane * 16, lds0 + (2 + buf) * kTileBytes + wave * 1024, i * 4096);
+        for (int u = 0; u < U; ++u) {
+            const int p = x < n && slot + 16 * u < span.hi ? table[(slot + 16 * u) >> kv.shift] : -1;
+            page[u] = (unsigned)p < (unsigned)kv.n_pages ? p : -1;
         }
     };
-    const float scale_log2 = a.scale * kLog2e;
+    // addresses of the units' first keys, 0: not there
+    const char* const pool = (const char*)kv.pool + kh * kv.block() * (int64_t)sizeof(T);
+    const int64_t page_bytes = kv.page_stride * (int64_t)sizeof(T);
+    auto bases = [&](int x, const int (&raw)[U], const char* (&base)[U]) {
+        const int slot = span.step_at(it0 + x) * KT;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = __builtin_amdgcn_readfirstlane(raw[u]);
+            base[u] = p < 0 ? nullptr : pool + p * page_bytes + ((slot + 16 * u) & ((1 << kv.shift) - 1)) * R::kBytes;
+        }
+    };
+    auto load_tile = [&](const char* const (&base)[U], bool values, uint32_t to) {
+        to += wave * 1024;
+        if constexpr (WIDE) {
+            if (!base[0]) return;  // uniform; what LDS holds there is masked, its values are cleared
+            const char* p = uniform(base[0] + (values ? to_values : 0));
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) dma_load16_at<false>(p, values ? (i * 4 + wave) * 1024 + lane * 16 : key_off[i], to, i * 4096);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) {
+                const int first = (i * 4 + wave) * kTok, u = first >> 4;
+                const char* p = base[0];
+#pragma unroll
+                for (int y = 1; y < U; ++y) p = u == y ? base[y] : p;
+                if (!p) continue;
+                p = uniform(p + (first & 15) * R::kBytes + (values ? to_values : 0));
+                dma_load16_at<false>(p, values ? lane * 16 : key_off[i], to, i * 4096);
+            }
+        }
+    };
+    auto gone_bits = [&](const char* const (&base)[U]) {  // bit u: unit u is not there
+        int bits = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) bits |= (base[u] == nullptr) << u;
+        return bits;
+    };
+    const float scale_log2 = a.scale * kLog2e, inv_scale = 1.0f / scale_log2;
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
 
-    if (it0 < it1) {
-        units(it0);
-        load_tile(0);
-    }
-    for (int it = it0; it < it1; ++it) {
-        const int buf = (it - it0) & 1, tok0 = span.step_at(it) * KT;
-        int gone = 0;  // bit u: the 16 tokens of unit u are not there
+    // A half tile's fragments of keys and of values are read well before they are multiplied: a read from LDS takes longer
+    // than a few products.
+    u32x4_t kf[MB][R::kFrags], vf[DH / 16];
+    auto read_keys = [&](const unsigned char* ks, int half) {
 #pragma unroll
-        for (int u = 0; u < MB; ++u) gone |= (unit[u] < 0) << u;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();  // the tile is there, and nobody reads the other buffer any more
-        asm volatile("" ::: "memory");
-        if (it + 1 < it1) {
-            units(it + 1);
-            load_tile(buf ^ 1);
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int j = 0; j < R::kFrags; ++j)
+                kf[mb][j] = *(const u32x4_t*)(ks + M::token(half * MB + mb, c16) * R::kBytes +
+                                              (((4 * j + g) ^ (R::turn(c16) & (R::kPieces - 1))) << 4));
+    };
+    auto read_values = [&](const unsigned char* vs, int half) {
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) vf[i] = *(const u32x4_t*)(vs + (M::unit(half, g, DH, 16 * i + c16) << 4));
+    };
+    auto scores = [&](f32x4_t (&sc)[NC][MB]) {
+#pragma unroll
+        for (int j = 0; j < R::kFrags; ++j)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) sc[c][mb] = M::mma(kf[mb][j], bq[c][j], j == 0 ? zero4 : sc[c][mb]);
+    };
+    auto add_values = [&](const u32x4_t (&p)[NC]) {
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) ot[c][i] = M::mma(vf[i], p[c], ot[c][i]);
+    };
+    // Before the exponentials of a step: what is not seen goes to -infinity, and ref moves up where a score is more than 2^8
+    // above it (rarely: weights up to 2^8 lose nothing).  A whole step 2^-k is exact, also for weights `due` that are
+    // rounded already and not yet multiplied with the values.
+    auto settle = [&](f32x4_t (&sc)[NC][MB], int tok, int gone, u32x4_t (&due)[NC]) {
+        if (gone || tok + KS > lim_min || (tok < from_max && tok + KS > span.sinks)) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = M::token(mb, 4 * g + i), j = tok + r;
+                        const bool seen = j < limit[c] && (j >= from[c] || j < span.sinks) && !(gone >> (r >> 4) & 1);
+                        sc[c][mb][i] = seen ? sc[c][mb][i] : -INFINITY;
+                    }
         }
-        const unsigned char* ks = smem + buf * kTileBytes;
-        unsigned char* vs = smem + (2 + buf) * kTileBytes;
-        // values that no row here sees may be anything: 0 x NaN must not reach a sum
-        if (gone || tok0 + KT > span.hi || (tok0 < span.lo && tok0 + KT > span.sinks)) {
-            constexpr int kUnitTok = 16 / (int)sizeof(T) > 4 ? 8 : 4;  // tokens of a 16-byte unit
-            for (int x = tid; x < kTileBytes / 16; x += 256) {
-                const int o = x * 16 / (8 * R::kBytes) * 8 + (sizeof(T) == 4 ? (x & 1) * 4 : 0);
-                T* e = (T*)(vs + x * 16);
+        float top[NC];
+        bool up = false;
 #pragma unroll
-                for (int y = 0; y < kUnitTok; ++y)
-                    if (!span.any(tok0 + o + y) || (gone >> ((o + y) >> 4) & 1)) e[y] = T{};
+        for (int c = 0; c < NC; ++c) {
+            top[c] = -INFINITY;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top[c] = fmaxf(top[c], sc[c][mb][i]);
+            up |= top[c] > bound[c];
+        }
+        if (__builtin_amdgcn_ballot_w64(up) == 0) return;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const float high = max_over_lane_groups(top[c]);  // the same decision in the four lanes of a column
+            const bool move = high > bound[c];
+            const float next = move ? __builtin_ceilf(high * scale_log2) : -minus_ref[c];
+            const float down = move && bound[c] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-next - minus_ref[c]);
+            minus_ref[c] = -next;
+            bound[c] = move ? (next + 8.f) * inv_scale : bound[c];
+            l[c] *= down;
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) ot[c][i] *= down;
+            due[c] = M::times(due[c], down);
+        }
+    };
+    auto weights = [&](f32x4_t (&sc)[NC][MB], u32x4_t (&p)[NC]) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][mb][i], scale_log2, minus_ref[c]));
+                    sc[c][mb][i] = w;
+                    l[c] += w;
+                }
+            p[c] = M::weights(sc[c]);
+        }
+    };
+
+    // Products and exponentials take turns, so that matrix and vector units both have something to do.
+    auto interleave = [&](u32x4_t (&p)[NC]) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(p[c]));  // the weights belong to this step, not to their use
+        constexpr int kMma = NC * (DH / 16) * (sizeof(T) == 2 ? 1 : 4), kExp = NC * MB * 4, kPer = (kMma + kExp - 1) / kExp;
+#pragma unroll
+        for (int i = 0; i < kExp; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+        }
+    };
+
+    // A pipeline over half tiles: while one half's exponentials run on the vector units, the matrix units multiply the half
+    // before with its values and the queries with the half after.  At tile x: values of x, keys of x + 1 are read; the
+    // loads of keys x + 2 and values x + 1 are on their way.
+    f32x4_t s0[NC][MB], s1[NC][MB];
+    u32x4_t p0[NC], p1[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) p1[c] = u32x4_t{0, 0, 0, 0};
+    int raw[U];
+    const char *base_k[U], *base_v[U];  // units of the tile whose keys (values) are loaded next
+    pages(0, raw);
+    bases(0, raw, base_v);
+    if (n > 0) load_tile(base_v, false, lds0);
+    int gone_next = 0, gone = 0;  // units of tiles x + 1 and x that are not there
+    pages(1, raw);
+    constexpr int kHalfUnits = WIDE ? 1 : KS / 16;
+    auto half_bits = [&](int bits, int half) { return WIDE ? (bits ? -1 : 0) : (bits >> (half * kHalfUnits)) & ((1 << kHalfUnits) - 1); };
+
+    // Start of tile x: waits for its keys and values' loads, starts the next ones.
+    auto turn = [&](int x) {
+        const int b = (x + 1) & 1;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // keys x + 1 and values x are there, and nobody reads keys x and values x - 1 any more
+        asm volatile("" ::: "memory");
+        bases(x + 2, raw, base_k);
+        gone = gone_next;
+        gone_next = gone_bits(base_v);
+        if (x + 2 < n) load_tile(base_k, false, lds0 + (b ^ 1) * kTileBytes);
+        if (x + 1 < n) load_tile(base_v, true, lds0 + (2 + b) * kTileBytes);
+#pragma unroll
+        for (int u = 0; u < U; ++u) base_v[u] = base_k[u];
+        pages(x + 3, raw);
+        if (x < 0) return;
+        // values that no row here sees may be anything: 0 x NaN must not reach a sum
+        const int tok = span.step_at(it0 + x) * KT;
+        if (gone || tok + KT > span.hi || (tok < span.lo && tok + KT > span.sinks)) {
+            unsigned char* vs = smem + (2 + (b ^ 1)) * kTileBytes;
+            constexpr int kUnitTok = sizeof(T) == 2 ? 8 : 4;  // tokens of a 16-byte unit
+            for (int y = tid; y < kTileBytes / 16; y += 256) {
+                const int o = y * 16 / (8 * R::kBytes) * 8 + (sizeof(T) == 4 ? (y & 1) * 4 : 0);
+                T* e = (T*)(vs + y * 16);
+#pragma unroll
+                for (int z = 0; z < kUnitTok; ++z)
+                    if (!span.any(tok + o + z) || (WIDE ? gone : gone >> ((o + z) >> 4) & 1)) e[z] = T{};
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         }
-        // nothing in this tile for the wave's rows
-        if (tok0 >= lim_max || (tok0 >= span.sinks && tok0 + KT <= from_min)) continue;
-        f32x4_t sc[NC][MB];
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int j = 0; j < R::kFrags; ++j) {
-                const u32x4_t k = *(const u32x4_t*)(ks + M::token(mb, c16) * R::kBytes +
-                                                    (((4 * j + g) ^ (R::turn(c16) & (R::kPieces - 1))) << 4));
-#pragma unroll
-                for (int c = 0; c < NC; ++c) sc[c][mb] = M::mma(k, bq[c][j], j == 0 ? zero4 : sc[c][mb]);
-            }
-        const bool need_mask = gone || tok0 + KT > lim_min || (tok0 < from_max && tok0 + KT > span.sinks);
-        u32x4_t p[NC][KG];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            float top = -INFINITY;
-            if (need_mask) {
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = M::token(mb, 4 * g + i), j = tok0 + r;
-                        const bool seen = j < limit[c] && (j >= from[c] || j < span.sinks) && !(gone >> (r >> 4) & 1);
-                        sc[c][mb][i] = seen ? sc[c][mb][i] : -INFINITY;
-                    }
-            }
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[c][mb][i]);
-            const float mnew = fmaxf(m[c], max_over_lane_groups(top));
-            const float ref = mnew == -INFINITY ? 0.f : mnew;
-            const float alpha = __builtin_amdgcn_exp2f((m[c] - ref) * scale_log2), nb = -ref * scale_log2;
-            float sum = 0.f;
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][mb][i], scale_log2, nb));
-                    sc[c][mb][i] = w;
-                    sum += w;
-                }
-            l[c] = l[c] * alpha + sum;
-            m[c] = mnew;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-                for (int i = 0; i < DH / 16; ++i) ot[c][i] *= alpha;
-            }
-#pragma unroll
-            for (int kk = 0; kk < KG; ++kk) p[c][kk] = M::weights(&sc[c][kk * (M::kGroup / 16)]);
+    };
+    if (n > 0) {
+        turn(-1);
+        read_keys(smem, 0);
+        scores(s0);
+        read_keys(smem, 1);
+        settle(s0, span.step_at(it0) * KT, half_bits(gone_next, 0), p1);
+        weights(s0, p0);
+        scores(s1);
+        for (int x = 0; x + 1 < n; ++x) {
+            turn(x);
+            const unsigned char *ks = smem + ((x + 1) & 1) * kTileBytes, *vs = smem + (2 + (x & 1)) * kTileBytes;
+            read_values(vs, 0);
+            read_keys(ks, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            settle(s1, span.step_at(it0 + x) * KT + KS, half_bits(gone, 1), p0);
+            __builtin_amdgcn_sched_barrier(0);
+            weights(s1, p1);
+            add_values(p0);
+            interleave(p1);
+            __builtin_amdgcn_sched_barrier(0);
+            read_values(vs, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            scores(s0);
+            __builtin_amdgcn_sched_barrier(0);
+            read_keys(ks, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            settle(s0, span.step_at(it0 + x + 1) * KT, half_bits(gone_next, 0), p1);
+            __builtin_amdgcn_sched_barrier(0);
+            weights(s0, p0);
+            add_values(p1);
+            interleave(p0);
+            __builtin_amdgcn_sched_barrier(0);
+            scores(s1);
         }
-#pragma unroll
-        for (int kk = 0; kk < KG; ++kk)
-#pragma unroll
-            for (int i = 0; i < DH / 16; ++i) {
-                const u32x4_t v = *(const u32x4_t*)(vs + (M::unit(kk, g, DH, 16 * i + c16) << 4));
-#pragma unroll
-                for (int c = 0; c < NC; ++c) ot[c][i] = M::mma(v, p[c][kk], ot[c][i]);
-            }
+        turn(n - 1);
+        const unsigned char* vs = smem + (2 + ((n - 1) & 1)) * kTileBytes;
+        read_values(vs, 0);
+        settle(s1, span.step_at(it0 + n - 1) * KT + KS, half_bits(gone, 1), p0);
+        weights(s1, p1);
+        add_values(p0);
+        read_values(vs, 1);
+        add_values(p1);
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const float total = sum_over_lane_groups(l[c]);
-        if (out_at[c] < 0) continue;
+        int col = qt * kCols + (wave * NC + c) * 16 + c16;
+        asm volatile("" : "+v"(col));  // worked out again rather than kept in registers for the whole loop
+        if (col >= n_cols) continue;
+        const int64_t row = cr.row0 + col / hpk;
+        const int head = kh * hpk + col % hpk;
         if (geo.n_split > 1) {
-            const int64_t piece = out_at[c] * geo.n_split + split;
+            const int64_t piece = (row * a.Hq + head) * geo.n_split + split;
             float* ml = geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH + 2 * piece;
-            if (g == 0) ml[0] = m[c] * scale_log2, ml[1] = total;
+            if (g == 0) ml[0] = total > 0.f ? -minus_ref[c] : -INFINITY, ml[1] = total;
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)(geo.part + piece * DH + 16 * i + 4 * g) = ot[c][i];
             continue;
         }
         const float inv = total > 0.f ? 1.0f / total : 0.f;
-        const int64_t row = out_at[c] / a.Hq;
-        T* out = (T*)a.out + row * a.out_stride + (out_at[c] - row * a.Hq) * DH;
+        T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH;
 #pragma unroll
         for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[16 * i + 4 * g + e] = from_f32<T>(ot[c][i][e] * inv);
-        if (a.lse && g == 0) a.lse[out_at[c]] = total > 0.f ? m[c] * a.scale + logf(total) : -INFINITY;
+        if (a.lse && g == 0) a.lse[row * a.Hq + head] = total > 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total) : -INFINITY;
     }
 }
 
@@ -936,10 +1065,10 @@ hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
     if (few_take(a))
         attn_few_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(a, geo);
-    else if (cols <= 64)
-        attn_tile_kernel<T, DH, 1><<<(unsigned)grid, 256, 0, s>>>(a, geo);
+    else if ((1 << a.kv.shift) >= 2 * Mat<T>::kGroup)
+        (cols <= 64 ? attn_tile_kernel<T, DH, 1, true> : attn_tile_kernel<T, DH, 2, true>)<<<(unsigned)grid, 256, 0, s>>>(a, geo);
     else
-        attn_tile_kernel<T, DH, 2><<<(unsigned)grid, 256, 0, s>>>(a, geo);
+        (cols <= 64 ? attn_tile_kernel<T, DH, 1, false> : attn_tile_kernel<T, DH, 2, false>)<<<(unsigned)grid, 256, 0, s>>>(a, geo);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || geo.n_split == 1) return e;
     const int64_t per = ceil_div64((int64_t)a.max_new * a.Hq * (DH / 4), 256);
