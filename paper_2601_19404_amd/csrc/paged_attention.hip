@@ -38,6 +38,7 @@ struct Mat;
 template <>
 struct Mat<bf16> {
     static constexpr int kGroup = 32;  // tokens of one product of weights and values
+    static constexpr int kLaneTok = 8;  // of which a lane holds so many, side by side
     // token of row c (0..15) of 16-token block mb: blocks 2 k and 2 k + 1 share 32 tokens, such that lane group g's rows
     // 4 g .. 4 g + 3 of both are the tokens 8 g .. 8 g + 7
     static __host__ __device__ constexpr int token(int mb, int c) { return 32 * (mb >> 1) + 8 * (c >> 2) + 4 * (mb & 1) + (c & 3); }
@@ -64,6 +65,7 @@ struct Mat<bf16> {
 template <>
 struct Mat<float> {
     static constexpr int kGroup = 16;
+    static constexpr int kLaneTok = 4;
     static __host__ __device__ constexpr int token(int mb, int c) { return 16 * mb + c; }
     static __device__ constexpr int row_c(int r) { return r & 15; }
     static __device__ inline f32x4_t mma(u32x4_t a, u32x4_t b, f32x4_t c) {
@@ -130,6 +132,9 @@ struct Span {
     __device__ int step_at(int i) const { return i < sink_steps ? i : lo_step + i - sink_steps; }
     __device__ bool any(int j) const { return j < hi && (j < sinks || j >= lo); }
 };
+
+// the lowest n bits (n below 0: none, above 32: all)
+__device__ inline uint32_t low_bits(int n) { return (uint32_t)((1ull << min(max(n, 0), 32)) - 1); }
 
 // ---------------------------------------------------------------------------
 // chunks
@@ -287,21 +292,41 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
 #pragma unroll
             for (int c = 0; c < NC; ++c) ot[c][i] = M::mma(vf[i], p[c], ot[c][i]);
     };
+    auto gone_mask = [&](int gone) -> uint32_t {  // bit r: token r of a half tile is not there
+        return WIDE ? (gone ? ~0u : 0u) : (gone & 1 ? 0xffffu : 0u) | (gone & 2 ? 0xffff0000u : 0u);
+    };
+    // Values that no row here sees may be anything, and 0 x NaN must not reach a sum: they are cleared on their way.
+    auto clear_unseen = [&](int tok, int gone) {
+        if (!gone && tok + KS <= span.hi && (tok >= span.lo || tok + KS <= span.sinks)) return;
+        const uint32_t seen = low_bits(span.hi - tok) & (low_bits(span.sinks - tok) | ~low_bits(span.lo - tok)) & ~gone_mask(gone);
+        const int mine = (int)(seen >> (M::kLaneTok * g));
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(mine, sizeof(T) == 2 ? 2 * d : d, 1);
+            if (sizeof(T) == 2) keep = (keep & 0xffffu) | ((uint32_t)__builtin_amdgcn_sbfe(mine, 2 * d + 1, 1) & 0xffff0000u);
+#pragma unroll
+            for (int i = 0; i < DH / 16; ++i) vf[i][d] &= keep;
+        }
+    };
     // Before the exponentials of a step: what is not seen goes to -infinity, and ref moves up where a score is more than 2^8
     // above it (rarely: weights up to 2^8 lose nothing).  A whole step 2^-k is exact, also for weights `due` that are
     // rounded already and not yet multiplied with the values.
     auto settle = [&](f32x4_t (&sc)[NC][MB], int tok, int gone, u32x4_t (&due)[NC]) {
         if (gone || tok + KS > lim_min || (tok < from_max && tok + KS > span.sinks)) {
+            const uint32_t sink = low_bits(span.sinks - tok), there = ~gone_mask(gone);
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+            for (int c = 0; c < NC; ++c) {
+                // bit r: the column sees the step's token r; a lane's tokens are M::kLaneTok * g + token(mb, i)
+                const uint32_t seen = low_bits(limit[c] - tok) & (sink | ~low_bits(from[c] - tok)) & there;
+                const uint32_t mine = seen >> (M::kLaneTok * g);
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int r = M::token(mb, 4 * g + i), j = tok + r;
-                        const bool seen = j < limit[c] && (j >= from[c] || j < span.sinks) && !(gone >> (r >> 4) & 1);
-                        sc[c][mb][i] = seen ? sc[c][mb][i] : -INFINITY;
+                        const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)mine, M::token(mb, i), 1);
+                        sc[c][mb][i] = __uint_as_float((keep & __float_as_uint(sc[c][mb][i])) | (~keep & 0xff800000u));
                     }
+            }
         }
         float top[NC];
         bool up = false;
@@ -388,23 +413,6 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
 #pragma unroll
         for (int u = 0; u < U; ++u) base_v[u] = base_k[u];
         pages(x + 3, raw);
-        if (x < 0) return;
-        // values that no row here sees may be anything: 0 x NaN must not reach a sum
-        const int tok = span.step_at(it0 + x) * KT;
-        if (gone || tok + KT > span.hi || (tok < span.lo && tok + KT > span.sinks)) {
-            unsigned char* vs = smem + (2 + (b ^ 1)) * kTileBytes;
-            constexpr int kUnitTok = sizeof(T) == 2 ? 8 : 4;  // tokens of a 16-byte unit
-            for (int y = tid; y < kTileBytes / 16; y += 256) {
-                const int o = y * 16 / (8 * R::kBytes) * 8 + (sizeof(T) == 4 ? (y & 1) * 4 : 0);
-                T* e = (T*)(vs + y * 16);
-#pragma unroll
-                for (int z = 0; z < kUnitTok; ++z)
-                    if (!span.any(tok + o + z) || (WIDE ? gone : gone >> ((o + z) >> 4) & 1)) e[z] = T{};
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        }
     };
     if (n > 0) {
         turn(-1);
@@ -418,9 +426,11 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
             turn(x);
             const unsigned char *ks = smem + ((x + 1) & 1) * kTileBytes, *vs = smem + (2 + (x & 1)) * kTileBytes;
             read_values(vs, 0);
-            read_keys(ks, 0);
             __builtin_amdgcn_sched_barrier(0);
-            settle(s1, span.step_at(it0 + x) * KT + KS, half_bits(gone, 1), p0);
+            const int tok = span.step_at(it0 + x) * KT;
+            settle(s1, tok + KS, half_bits(gone, 1), p0);
+            clear_unseen(tok, half_bits(gone, 0));
+            read_keys(ks, 0);
             __builtin_amdgcn_sched_barrier(0);
             weights(s1, p1);
             add_values(p0);
@@ -430,9 +440,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
             __builtin_amdgcn_sched_barrier(0);
             scores(s0);
             __builtin_amdgcn_sched_barrier(0);
-            read_keys(ks, 1);
-            __builtin_amdgcn_sched_barrier(0);
             settle(s0, span.step_at(it0 + x + 1) * KT, half_bits(gone_next, 0), p1);
+            clear_unseen(tok + KS, half_bits(gone, 1));
+            read_keys(ks, 1);
             __builtin_amdgcn_sched_barrier(0);
             weights(s0, p0);
             add_values(p1);
@@ -442,11 +452,14 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         }
         turn(n - 1);
         const unsigned char* vs = smem + (2 + ((n - 1) & 1)) * kTileBytes;
+        const int tok = span.step_at(it0 + n - 1) * KT;
         read_values(vs, 0);
-        settle(s1, span.step_at(it0 + n - 1) * KT + KS, half_bits(gone, 1), p0);
+        settle(s1, tok + KS, half_bits(gone, 1), p0);
+        clear_unseen(tok, half_bits(gone, 0));
         weights(s1, p1);
         add_values(p0);
         read_values(vs, 1);
+        clear_unseen(tok + KS, half_bits(gone, 1));
         add_values(p1);
     }
 #pragma unroll
@@ -667,15 +680,34 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeo
     const int64_t row = cr.row0 + i, at = row * a.Hq + head, piece = at * n_split;
     const float* ml = geo.part + (int64_t)a.n_rows * a.Hq * n_split * DH + 2 * piece;
     const float* po = geo.part + piece * DH + ch;
-    float top = -INFINITY;
-    for (int p = 0; p < n_split; ++p) top = fmaxf(top, ml[2 * p]);
-    float total = 0.f;
+    // eight pieces' loads at once: what counts is the number of times that memory is waited for
+    constexpr int kAtOnce = 8;
+    float top = -INFINITY, total = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < n_split; ++p) {
-        if (ml[2 * p] == -INFINITY) continue;  // saw nothing
-        const float wgt = __builtin_amdgcn_exp2f(ml[2 * p] - top);
-        total += wgt * ml[2 * p + 1];
-        o += wgt * *(const f32x4_t*)(po + (int64_t)p * DH);
+    for (int p0 = 0; p0 < n_split; p0 += kAtOnce) {
+        float m[kAtOnce], l[kAtOnce];
+        f32x4_t v[kAtOnce];
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            const int p = min(p0 + y, n_split - 1);
+            m[y] = ml[2 * p], l[y] = ml[2 * p + 1];
+            v[y] = *(const f32x4_t*)(po + (int64_t)p * DH);
+        }
+        float next = top;
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) next = fmaxf(next, m[y]);
+        if (next == -INFINITY) continue;  // nothing seen so far
+        const float down = __builtin_amdgcn_exp2f(top - next);
+        top = next;
+        total *= down;
+        o *= down;
+#pragma unroll
+        for (int y = 0; y < kAtOnce; ++y) {
+            if (p0 + y >= n_split || m[y] == -INFINITY) continue;  // a piece that saw nothing holds anything
+            const float wgt = __builtin_amdgcn_exp2f(m[y] - top);
+            total += wgt * l[y];
+            o += wgt * v[y];
+        }
     }
     const float inv = total > 0.f ? 1.0f / total : 0.f;
     T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH + ch;
@@ -716,23 +748,34 @@ __device__ inline int load_keys(const PagedKv& kv, int s, int kh, int tok0, int 
     return gone;
 }
 
-// Tokens' sums to where they go: lanes 0-15 hold the tokens tok0 + 16 mb + lane.
+// A lane's token of the wave's, and where its score so far comes from; the lanes beyond the tokens have none.
+struct ScoreSlot {
+    int64_t at;
+    bool there;
+    float before;
+    __device__ ScoreSlot(const PagedScoreArgs& b, int combo, int tok0, int n_tok, int len) {
+        const int lane = threadIdx.x & 63;
+        at = combo * b.score_stride + tok0 + lane;
+        there = lane < n_tok && tok0 + lane < len;
+        before = there && b.score_in ? b.score_in[at] : 0.f;
+    }
+};
+// The sums of a wave's tokens to where they go: lane l writes token l.
 template <int MB>
-__device__ inline void store_scores(const PagedScoreArgs& b, const ScoreGeom& geo, int combo, int split, int tok0, int len, int gone,
-                                    const float (&acc)[MB]) {
-    const int lane = threadIdx.x & 63;
+__device__ inline void store_scores(const PagedScoreArgs& b, const ScoreGeom& geo, int combo, int split, const ScoreSlot& slot, int tok0,
+                                    int gone, const float (&acc)[MB]) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float sum = 0.f;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
-        const float sum = (gone >> mb & 1) ? 0.f : sum_over_lane_groups(acc[mb]);
-        const int j = tok0 + 16 * mb + lane;
-        if (lane >= 16 || j >= len) continue;
-        if (geo.n_split > 1) {
-            geo.part[((int64_t)split * geo.combos + combo) * b.at.max_len + j] = sum;
-        } else {
-            const int64_t at = combo * b.score_stride + j;
-            b.score_out[at] = (b.score_in ? b.score_in[at] : 0.f) + sum;
-        }
+        const float x = sum_over_lane_groups(acc[mb]);  // of token 16 mb + lane % 16
+        if (g == mb && !(gone >> mb & 1)) sum = x;
     }
+    if (!slot.there) return;
+    if (geo.n_split > 1)
+        geo.part[((int64_t)split * geo.combos + combo) * b.at.max_len + tok0 + (threadIdx.x & 63)] = sum;
+    else
+        b.score_out[slot.at] = slot.before + sum;
 }
 
 template <typename T, int DH>
@@ -750,15 +793,16 @@ __global__ __launch_bounds__(256) void score_few_kernel(PagedScoreArgs b, ScoreG
     const ChunkRows cr = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
     const int hpk = a.Hq / kv.Hkv, n_cols = cr.n * hpk;
     const Span span(cr.slot0, cr.slot0 + cr.n - 1, a.window, a.sinks, 16);
+    const bool some = n_cols > 0 && tok0 < span.hi && (tok0 < span.sinks || tok0 + 16 * MB > span.lo);
+    if (!some && b.score_in == b.score_out) return;
     float acc[MB];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) acc[mb] = 0.f;
-    const bool some = n_cols > 0 && tok0 < span.hi && (tok0 < span.sinks || tok0 + 16 * MB > span.lo);
-    if (!some && b.score_in == b.score_out) return;
     int gone = 0;
+    u32x4_t k[MB][R::kFrags], q[R::kFrags];
+    if (some) gone = load_keys<T, DH>(kv, s, kh, tok0, len, k);
+    const ScoreSlot slot(b, combo, tok0, 16 * MB, len);
     if (some) {
-        u32x4_t k[MB][R::kFrags], q[R::kFrags];
-        gone = load_keys<T, DH>(kv, s, kh, tok0, len, k);
         const int col = c16 < n_cols ? c16 : 0;
         const T* qp = (const T*)a.q + (int64_t)(cr.row0 + col / hpk) * a.q_stride + (int64_t)(kh * hpk + col % hpk) * DH;
 #pragma unroll
@@ -787,7 +831,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(PagedScoreArgs b, ScoreG
             }
         }
     }
-    store_scores<MB>(b, geo, combo, 0, tok0, len, gone, acc);
+    store_scores<MB>(b, geo, combo, 0, slot, tok0, gone, acc);
 }
 
 template <typename T, int DH>
@@ -908,7 +952,7 @@ __global__ __launch_bounds__(256, 2) void score_tile_kernel(PagedScoreArgs b, Sc
         }
         if (more && wave == 0) shifts[buf ^ 1][lane] = lse_next, slots[buf ^ 1][lane] = slot_next;
     }
-    store_scores<MB>(b, geo, combo, split, tok0, len, gone, acc);
+    store_scores<MB>(b, geo, combo, split, ScoreSlot(b, combo, tok0, 16 * MB, len), tok0, gone, acc);
 }
 
 __global__ __launch_bounds__(256) void score_join_kernel(PagedScoreArgs b, ScoreGeom geo) {

@@ -3,9 +3,11 @@
 //
 //  * append_kernel: rows of keys and values to the last slots of their sequences.  A workgroup takes the eight slots of one
 //    octet, in which a page keeps its values, so that a full octet leaves as one 16- or 32-byte unit per channel.
-//  * evict_select_kernel: which slots stay, per (sequence, KV head): the radix select of the budget's last score, then one
-//    pass that lists the slots in order.
+//  * evict_select_kernel: which slots stay, per (sequence, KV head): a search for the score of the last one that the budget
+//    has room for, then one pass that lists the slots in order.
 //  * evict_move_kernel: the kept tokens' keys and values to the first slots of other pages.
+#include <algorithm>
+
 #include "kernels.hpp"
 
 namespace rpo {
@@ -69,40 +71,46 @@ __global__ __launch_bounds__(256) void append_kernel(PagedAppendArgs a, bool wid
 
 // ---------------------------------------------------------------------------
 // select.  A score's rank is that of its bits, turned so that unsigned order is the order of the numbers (NaN lowest,
-// -0 equal to 0).  Three passes of 11, 11 and 10 bits find the bits of the last score that the budget has room for; integer
-// counts alone decide, so the result does not depend on any order.  Thread t owns the t-th stretch of the slots, so that one
-// scan over the threads gives every stretch the number of ties and of kept slots before it.
+// -0 equal to 0).  The rank of the last score that the budget has room for lies between the lowest and the highest one; a
+// histogram over 2048 equal parts of that range says in which part, and so on until the part is one rank: three passes at
+// most, and few scores meet in one counter.  Integer counts alone decide, so the result does not depend on any order.
+// A wave owns a stretch of the slots, 64 side by side at a time, and counts with ballots.  EACH > 0: that many times 64, which
+// stay in registers; 0: longer rows are read again for every pass.  Rows of 16384: 33 -> 12 us a launch against fixed digits of 11 bits read from memory each time.
 // ---------------------------------------------------------------------------
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kBins = 2048;
+
+constexpr uint32_t kAlways = ~0u;
 
 __device__ inline uint32_t rank_bits(float x) {
-    if (x != x) return 0;
+    if (x != x) return 1;
     const uint32_t u = __float_as_uint(x + 0.0f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// exclusive sums of two counts over the threads of the workgroup
-__device__ inline int2 scan_pairs(int2 v, int2* part) {
+// exclusive sum over the threads of the workgroup
+__device__ inline int scan(int v, int* part) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int2 inc = v;
+    int inc = v;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(inc.x, o, 64), y = __shfl_up(inc.y, o, 64);
-        if (lane >= o) inc.x += x, inc.y += y;
+        const int x = __shfl_up(inc, o, 64);
+        if (lane >= o) inc += x;
     }
     if (lane == 63) part[wave] = inc;
     __syncthreads();
-    int2 base = {0, 0};
-    for (int w = 0; w < wave; ++w) base.x += part[w].x, base.y += part[w].y;
-    __syncthreads();
-    return {base.x + inc.x - v.x, base.y + inc.y - v.y};
+    int base = 0;
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) base += w < wave ? part[w] : 0;
+    return base + inc - v;
 }
 
+template <int EACH>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictArgs a) {
-    __shared__ int hist[2048];
-    __shared__ int2 part[kSelThreads / 64];
+    __shared__ int hist[kBins];
+    __shared__ int part[kSelWaves], more[kSelWaves];
+    __shared__ uint32_t ends[2][kSelWaves];
     __shared__ int pick[2];
-    const int tid = threadIdx.x, h = blockIdx.x, s = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.x, s = blockIdx.y;
     const int64_t row = (int64_t)s * a.src.Hkv + h;
     const float* score = a.score + row * a.score_stride;
     float* score_out = a.score_out ? a.score_out + row * a.score_out_stride : nullptr;
@@ -120,63 +128,99 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(PagedEvictArg
         return;
     }
     const int m0 = a.sinks, m1 = L - a.recent;  // the slots that compete
-    int need = a.budget - a.sinks - a.recent;   // 0 <= need < m1 - m0
-    uint32_t prefix = 0;
-    int done = 0;  // leading bits of the threshold known
+    constexpr int kBlock = EACH ? EACH : 16;    // scores asked for at once
+    const int per = EACH ? EACH : (L + kSelThreads - 1) / kSelThreads;
+    const int j0 = wave * per * 64 + lane;      // a lane's e-th slot: j0 + 64 e
+    // ranks: 0 beyond the row, ~0 for the slots that stay whatever their score, both outside what scores can have
+    float v[kBlock];
+    uint32_t rank[kBlock];
+    auto fetch = [&](int e0) {
+#pragma unroll
+        for (int e = 0; e < kBlock; ++e) v[e] = e0 + e < per && j0 + 64 * (e0 + e) < L ? score[j0 + 64 * (e0 + e)] : 0.f;
+#pragma unroll
+        for (int e = 0; e < kBlock; ++e) {
+            const int j = j0 + 64 * (e0 + e);
+            rank[e] = e0 + e >= per || j >= L ? 0 : j < m0 || j >= m1 ? kAlways : rank_bits(v[e]);
+        }
+    };
+    if constexpr (EACH > 0) fetch(0);
+    auto each = [&](auto f) {  // f(slot, rank, score), all lanes together
+        for (int e0 = 0; e0 < (EACH ? 1 : per); e0 += kBlock) {
+            if constexpr (EACH == 0) fetch(e0);
+#pragma unroll
+            for (int e = 0; e < kBlock; ++e) f(j0 + 64 * (e0 + e), rank[e], v[e]);
+        }
+    };
+    int need = a.budget - a.sinks - a.recent;  // 0 <= need < m1 - m0
+    uint32_t lo = kAlways - 1, hi = 0;  // of the ranks that compete; in the end the rank of the last one kept
     if (need > 0) {
-        for (int pass = 0; pass < 3; ++pass) {
-            const int bits = pass < 2 ? 11 : 10, shift = 32 - done - bits;
-            for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
-            __syncthreads();
-            for (int j = m0 + tid; j < m1; j += kSelThreads) {
-                const uint32_t key = rank_bits(score[j]);
-                if (done == 0 || (key >> (32 - done)) == prefix) atomicAdd(&hist[(key >> shift) & ((1 << bits) - 1)], 1);
-            }
+        for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+        each([&](int, uint32_t k, float) {
+            if (k - 1 < kAlways - 1) lo = min(lo, k), hi = max(hi, k);
+        });
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+        if (lane == 0) ends[0][wave] = lo, ends[1][wave] = hi;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kSelWaves; ++w) lo = min(lo, ends[0][w]), hi = max(hi, ends[1][w]);
+        while (lo < hi) {  // uniform; the range shrinks to a 2048th each time
+            const int shift = max(0, 32 - 11 - __builtin_clz(hi - lo));
+            each([&](int, uint32_t k, float) {
+                const int bin = k - lo <= hi - lo ? (int)((k - lo) >> shift) : -1;
+                // lanes that fall into the first one's bin (many scores are equal, zeros for instance) count at once
+                const int same = __builtin_amdgcn_readfirstlane(bin);
+                const uint64_t with = __builtin_amdgcn_ballot_w64(bin == same);
+                if (bin != same) {
+                    if (bin >= 0) atomicAdd(&hist[bin], 1);
+                } else if (bin >= 0 && lane == __builtin_ctzll(with)) {
+                    atomicAdd(&hist[bin], __builtin_popcountll(with));
+                }
+            });
             __syncthreads();
             // from the highest bin down: the bin in which the need-th score lies.  Thread t holds bins 2047 - 2 t and
             // 2046 - 2 t, so that sums over the threads before it are sums over the bins above.
-            const int hi = hist[2047 - 2 * tid], lo = hist[2046 - 2 * tid];
-            const int before = scan_pairs({hi + lo, 0}, part).x;
-            if (before < need && need <= before + hi + lo) {
-                const bool first = need <= before + hi;
-                pick[0] = first ? 2047 - 2 * tid : 2046 - 2 * tid;
-                pick[1] = first ? before : before + hi;
+            const int up = hist[kBins - 1 - 2 * tid], down = hist[kBins - 2 - 2 * tid];
+            hist[kBins - 1 - 2 * tid] = hist[kBins - 2 - 2 * tid] = 0;
+            const int before = scan(up + down, part);
+            if (before < need && need <= before + up + down) {
+                const bool first = need <= before + up;
+                pick[0] = first ? kBins - 1 - 2 * tid : kBins - 2 - 2 * tid;
+                pick[1] = first ? before : before + up;
             }
             __syncthreads();
-            prefix = (prefix << bits) | (uint32_t)pick[0];
             need -= pick[1];
-            done += bits;
-            __syncthreads();
+            lo += (uint32_t)pick[0] << shift;
+            hi = min(hi, lo + ((1u << shift) - 1));
         }
     }
-    // prefix: the threshold; need: how many of the slots at it stay, the lowest ones
-    const bool any = a.budget > a.sinks + a.recent;
-    const int per = (L + kSelThreads - 1) / kSelThreads;
-    const int j0 = min(tid * per, L), j1 = min(j0 + per, L);
-    int2 cnt = {0, 0};  // kept for sure, at the threshold
-    for (int j = j0; j < j1; ++j) {
-        if (j < m0 || j >= m1) {
-            ++cnt.x;
-        } else if (any) {
-            const uint32_t key = rank_bits(score[j]);
-            cnt.x += key > prefix;
-            cnt.y += key == prefix;
-        }
-    }
-    const int2 base = scan_pairs(cnt, part);
-    int ties = base.y, at = base.x + min(base.y, need);
-    for (int j = j0; j < j1; ++j) {
-        bool keep = j < m0 || j >= m1;
-        if (!keep && any) {
-            const uint32_t key = rank_bits(score[j]);
-            keep = key > prefix || (key == prefix && ties++ < need);
-        }
+    // lo: the threshold; need: how many of the slots at it stay, the lowest ones.  Every wave counts what it keeps for sure
+    // and what lies at the threshold, then places its own behind those of the waves before it.
+    int n_sure = 0, n_tied = 0;
+    each([&](int, uint32_t k, float) {
+        n_sure += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > lo));
+        n_tied += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == lo));
+    });
+    __syncthreads();
+    if (lane == 0) part[wave] = n_sure, more[wave] = n_tied;
+    __syncthreads();
+    int at = 0, ties = 0;
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) at += w < wave ? part[w] : 0, ties += w < wave ? more[w] : 0;
+    at += min(ties, need);
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    each([&](int j, uint32_t k, float x) {
+        const uint64_t t = __builtin_amdgcn_ballot_w64(k == lo);
+        const bool keep = k > lo || (k == lo && ties + __builtin_popcountll(t & below) < need);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(keep);
+        const int to = at + __builtin_popcountll(m & below);
         if (keep) {
-            kept[at] = j;
-            if (score_out) score_out[at] = score[j];
-            ++at;
+            kept[to] = j;
+            if (score_out) score_out[to] = x;
         }
-    }
+        at += __builtin_popcountll(m);
+        ties += __builtin_popcountll(t);
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -263,7 +307,12 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s) {
 
 hipError_t launch_paged_evict(const PagedEvictArgs& a, hipStream_t s) {
     if (a.src.n_seqs <= 0) return hipSuccess;
-    evict_select_kernel<<<dim3(a.src.Hkv, a.src.n_seqs), kSelThreads, 0, s>>>(a);
+    const int64_t longest = std::min(a.score_stride, (int64_t)a.src.table_stride << a.src.shift);
+    auto select = longest <= 4 * kSelThreads    ? evict_select_kernel<4>
+                  : longest <= 16 * kSelThreads ? evict_select_kernel<16>
+                  : longest <= 32 * kSelThreads ? evict_select_kernel<32>
+                                                : evict_select_kernel<0>;
+    select<<<dim3(a.src.Hkv, a.src.n_seqs), kSelThreads, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const bool wide = a.src.dh * dtype_size(a.src.dtype) % 16 == 0;
