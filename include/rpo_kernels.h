@@ -87,7 +87,7 @@ typedef struct {
 int rpo_batch_kv(const struct rpo_batch *b, int32_t layer, rpo_paged_kv *out);
 
 /* The rows of a call (below): sequence s has rows cu_rows_dev[s] .. cu_rows_dev[s + 1] - 1 of the row arrays, any number from
- * 0 up to max_new (the longest; a host bound that sizes the launch: rows of a sequence beyond it are not looked at).  They
+ * 0 up to max_new (the longest, below 2^26; a host bound that sizes the launch: rows of a sequence beyond it are not looked at).  They
  * are the last tokens of its cache: with n rows, row i sits at slot len - n + i.  cu_rows_dev: device int32 [n_seqs + 1],
  * not decreasing.  Rows of the arrays that belong to no sequence are left as they were.
  *

@@ -473,18 +473,18 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         if (geo.n_split > 1) {
             const int64_t piece = (row * a.Hq + head) * geo.n_split + split;
             float* ml = geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH + 2 * piece;
-            if (g == 0) ml[0] = total > 0.f ? -minus_ref[c] : -INFINITY, ml[1] = total;
+            if (g == 0) ml[0] = total != 0.f ? -minus_ref[c] : -INFINITY, ml[1] = total;
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)(geo.part + piece * DH + 16 * i + 4 * g) = ot[c][i];
             continue;
         }
-        const float inv = total > 0.f ? 1.0f / total : 0.f;
+        const float inv = total != 0.f ? 1.0f / total : 0.f;
         T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH;
 #pragma unroll
         for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[16 * i + 4 * g + e] = from_f32<T>(ot[c][i][e] * inv);
-        if (a.lse && g == 0) a.lse[row * a.Hq + head] = total > 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total) : -INFINITY;
+        if (a.lse && g == 0) a.lse[row * a.Hq + head] = total != 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total) : -INFINITY;
     }
 }
 
@@ -659,11 +659,11 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
             if (ch == 0) ml[0] = top, ml[1] = total;
             continue;
         }
-        const float inv = total > 0.f ? 1.0f / total : 0.f;
+        const float inv = total != 0.f ? 1.0f / total : 0.f;
         T* out = (T*)a.out + row * a.out_stride + head * DH + ch;
 #pragma unroll
         for (int e = 0; e < 4; ++e) out[e] = from_f32<T>(o[e] * inv);
-        if (a.lse && ch == 0) a.lse[at] = total > 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
+        if (a.lse && ch == 0) a.lse[at] = total != 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
     }
 }
 
@@ -709,11 +709,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeo
             o += wgt * v[y];
         }
     }
-    const float inv = total > 0.f ? 1.0f / total : 0.f;
+    const float inv = total != 0.f ? 1.0f / total : 0.f;
     T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH + ch;
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] = from_f32<T>(o[e] * inv);
-    if (a.lse && ch == 0) a.lse[at] = total > 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
+    if (a.lse && ch == 0) a.lse[at] = total != 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -835,7 +835,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(PagedScoreArgs b, ScoreG
 }
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void score_tile_kernel(PagedScoreArgs b, ScoreGeom geo) {
+__global__ __launch_bounds__(256, 3) void score_tile_kernel(PagedScoreArgs b, ScoreGeom geo) {
     using R = Row<T, DH>;
     using M = Mat<T>;
     constexpr int MB = kScoreBlocks<T>, QT = 64;      // query columns of a tile
@@ -1014,14 +1014,14 @@ __global__ __launch_bounds__(64) void attn_rows_kernel(PagedAttnArgs a) {
             o[u] = acc;
         }
     }
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
     T* out = (T*)a.out + row * a.out_stride + (int64_t)hq * dh;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int d = lane + 64 * u;
         if (d < dh) out[d] = from_f32<T>(o[u] * inv);
     }
-    if (a.lse && lane == 0) a.lse[row * a.Hq + hq] = l > 0.f ? m + logf(l) : -INFINITY;
+    if (a.lse && lane == 0) a.lse[row * a.Hq + hq] = l != 0.f ? m + logf(l) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -1069,12 +1069,21 @@ __global__ __launch_bounds__(256) void score_rows_kernel(PagedScoreArgs b) {
     }
 }
 
+constexpr int64_t kMaxGrid = 0xffffff;  // workgroups of 256 threads: a launch has fewer than 2^32 threads
+
 // Whether the matrix kernels take a call: fragments are 16 aligned bytes, offsets inside a tile of rows 32 bits.
 bool tiles_take(const PagedAttnArgs& a) {
     const int es = (int)dtype_size(a.kv.dtype);
     return a.path != 1 && (a.kv.dh == 32 || a.kv.dh == 64 || a.kv.dh == 128) && (uintptr_t)a.q % 16 == 0 && a.q_stride * es % 16 == 0;
 }
-bool few_take(const PagedAttnArgs& a) { return (int64_t)a.max_new * (a.Hq / a.kv.Hkv) <= 16; }
+// Up to 16 columns per KV head go to the kernel that streams tokens to registers: us a call, tiles / it, one token over
+// 4 x 8000 19.1 / 14.7, over 32 x 1750 in fp32 43.6 / 27.7; 14 columns over 2 x 4000 13.6 / 15.1.
+int64_t n_cols(const PagedAttnArgs& a) { return (int64_t)a.max_new * (a.Hq / a.kv.Hkv); }
+bool few_take(const PagedAttnArgs& a) { return n_cols(a) <= 16; }
+// Columns of a tile: 64 where they hold a chunk (128 / 64: 64 x 8 rows of 1.5B heads over 2100 tokens 36.4 / 31.4 us, 26 x 9
+// rows in fp32 over 80 tokens 26.7 / 14.9), else 128, which read every fragment of keys and values for twice the columns.
+int tile_cols(const PagedAttnArgs& a) { return n_cols(a) <= 64 ? 64 : 128; }
+int64_t attn_tiles(const PagedAttnArgs& a) { return few_take(a) ? 1 : ceil_div64(n_cols(a), tile_cols(a)); }
 
 // Slots that the rows of a chunk see at most.
 int most_seen(const PagedAttnArgs& a) {
@@ -1082,18 +1091,19 @@ int most_seen(const PagedAttnArgs& a) {
     return (int)(w < a.max_len ? w : a.max_len);
 }
 
-// Pieces that the tokens of a sequence are cut into, so that a few hundred workgroups work; none shorter than eight steps of
-// the few-column kernel (two a wave) or two tiles.
+// Pieces that the tokens of a sequence are cut into: as many as the two workgroups that a CU holds leave room for (one more
+// round for the rest costs more than it gives: fp32, 8 sequences of 200 rows, 304 workgroups, in two pieces 250 us, whole 190),
+// but none so short that the partial sums, 4 bytes a channel and query column, outweigh the tokens: eight steps of the
+// few-column kernel (two a wave; with four, a token over 2176 took 10.8 instead of 10.4 us), two tokens for every column of a
+// tile (7B heads, 2 x 20 rows over 4000 tokens: 128 / 256 / 512 tokens for 128 columns 20.0 / 19.4 / 22.8 us).
 int attn_splits(const PagedAttnArgs& a) {
     if (a.kv.n_seqs < 1 || a.max_new < 1 || a.max_len < 1 || !tiles_take(a)) return 1;
-    const int hpk = a.Hq / a.kv.Hkv, es = (int)dtype_size(a.kv.dtype);
     const bool few = few_take(a);
-    const int64_t tiles = few ? 1 : ceil_div64((int64_t)a.max_new * hpk, (int64_t)a.max_new * hpk <= 64 ? 64 : 128);
-    const int64_t groups = (int64_t)a.kv.n_seqs * a.kv.Hkv * tiles;
-    const int step = few ? 8 * (es == 2 ? 32 : 16) : 2 * (es == 2 ? 64 : 32);
-    const int64_t want = ceil_div64(512, groups), cap = most_seen(a) / step > 0 ? most_seen(a) / step : 1;
-    const int64_t n = want < cap ? want : cap;
-    return (int)(n < 64 ? n : 64);
+    const int64_t groups = (int64_t)a.kv.n_seqs * a.kv.Hkv * attn_tiles(a);
+    const int step = few ? 8 * (a.kv.dtype == kF32 ? Mat<float>::kGroup : Mat<bf16>::kGroup) : 2 * tile_cols(a);
+    const int64_t room = 512 / groups, cap = most_seen(a) / step;
+    const int64_t n = room < cap ? room : cap;
+    return (int)(n < 1 ? 1 : n < 64 ? n : 64);
 }
 
 template <typename T, int DH>
@@ -1102,22 +1112,17 @@ hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
     geo.combos = a.kv.n_seqs * a.kv.Hkv;
     geo.n_split = a.ws ? attn_splits(a) : 1;
     geo.part = (float*)a.ws;
-    const int hpk = a.Hq / a.kv.Hkv;
-    const int64_t cols = (int64_t)a.max_new * hpk;
-    const int64_t tiles = few_take(a) ? 1 : ceil_div64(cols, cols <= 64 ? 64 : 128);
-    const int64_t grid = tiles * geo.combos * geo.n_split;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
-    if (few_take(a))
-        attn_few_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(a, geo);
-    else if ((1 << a.kv.shift) >= 2 * Mat<T>::kGroup)
-        (cols <= 64 ? attn_tile_kernel<T, DH, 1, true> : attn_tile_kernel<T, DH, 2, true>)<<<(unsigned)grid, 256, 0, s>>>(a, geo);
-    else
-        (cols <= 64 ? attn_tile_kernel<T, DH, 1, false> : attn_tile_kernel<T, DH, 2, false>)<<<(unsigned)grid, 256, 0, s>>>(a, geo);
+    const int64_t grid = attn_tiles(a) * geo.combos * geo.n_split;
+    const int64_t join = ceil_div64((int64_t)a.max_new * a.Hq * (DH / 4), 256);
+    if (grid > kMaxGrid || join > kMaxGrid) return hipErrorInvalidValue;
+    const bool wide = (1 << a.kv.shift) >= 2 * Mat<T>::kGroup, small = tile_cols(a) == 64;
+    auto kernel = few_take(a) ? attn_few_kernel<T, DH>
+                  : wide      ? (small ? attn_tile_kernel<T, DH, 1, true> : attn_tile_kernel<T, DH, 2, true>)
+                              : (small ? attn_tile_kernel<T, DH, 1, false> : attn_tile_kernel<T, DH, 2, false>);
+    kernel<<<(unsigned)grid, 256, 0, s>>>(a, geo);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || geo.n_split == 1) return e;
-    const int64_t per = ceil_div64((int64_t)a.max_new * a.Hq * (DH / 4), 256);
-    if (per > 0x7fffffff) return hipErrorInvalidValue;
-    attn_join_kernel<T, DH><<<dim3((unsigned)per, a.kv.n_seqs), 256, 0, s>>>(a, geo);
+    attn_join_kernel<T, DH><<<dim3((unsigned)join, a.kv.n_seqs), 256, 0, s>>>(a, geo);
     return hipGetLastError();
 }
 
@@ -1126,14 +1131,16 @@ bool score_tiles_take(const PagedScoreArgs& b) {
     return tiles_take(b.at) && b.at.q_stride < ((int64_t)1 << 30) / 66 / (int)dtype_size(b.at.kv.dtype);
 }
 
-// Pieces that the query columns are cut into: about four workgroups per CU, none of fewer than eight tiles.
+// Pieces that the query columns are cut into: about four workgroups per CU (two: 7B heads, 1 x 8000 rows 448 instead of 279 us,
+// for want of balance between the first and the last tokens), none of fewer than three tiles (eight / three: 8 x 150 rows of
+// 1.5B heads over 2100 tokens 44.7 / 23.7 us, 500 rows over 4000 32.5 / 26.0).
 int score_splits(const PagedScoreArgs& b) {
     const PagedAttnArgs& a = b.at;
     if (a.kv.n_seqs < 1 || a.max_new < 1 || a.max_len < 1 || !score_tiles_take(b) || few_take(a)) return 1;
     const int64_t rows = a.window && a.window + (int64_t)256 < a.max_new ? a.window + 256 : a.max_new;
     const int64_t tiles = ceil_div64(rows * (a.Hq / a.kv.Hkv), 64);
     const int64_t groups = (int64_t)a.kv.n_seqs * a.kv.Hkv * ceil_div(a.max_len, a.kv.dtype == kF32 ? 128 : 256);
-    const int64_t want = ceil_div64(1024, groups), cap = tiles / 8 > 0 ? tiles / 8 : 1;
+    const int64_t want = ceil_div64(1024, groups), cap = tiles / 3 > 0 ? tiles / 3 : 1;
     const int64_t n = want < cap ? want : cap;
     return (int)(n < 16 ? n : 16);
 }
@@ -1146,7 +1153,7 @@ hipError_t launch_score_tiles(const PagedScoreArgs& b, hipStream_t s) {
     geo.n_split = a.ws ? score_splits(b) : 1;
     geo.part = (float*)a.ws;
     const int64_t grid = (int64_t)ceil_div(a.max_len, 64 * kScoreBlocks<T>) * geo.combos * geo.n_split;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    if (grid > kMaxGrid) return hipErrorInvalidValue;
     if (few_take(a))
         score_few_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(b, geo);
     else

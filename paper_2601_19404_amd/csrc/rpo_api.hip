@@ -1249,6 +1249,7 @@ extern "C" int rpo_gemm_nt_noalloc(const void* a_dev, int64_t lda, const void* w
 namespace {
 
 constexpr int kMaxSeqs = 65535;  // grid dimensions y and z
+constexpr int kMaxNew = 1 << 26;  // workgroups of 64 threads along x: a launch has fewer than 2^32 threads
 
 // The checks of a cache that the host can make; fills in the kernels' form of it.
 int paged_kv(const char* who, const rpo_paged_kv* kv, bool needs_len, PagedKv* o) {
@@ -1284,8 +1285,8 @@ int paged_kv(const char* who, const rpo_paged_kv* kv, bool needs_len, PagedKv* o
 
 int rows_args(const char* who, const int32_t* cu, int n_rows, int max_new) {
     if (!cu) return fail(RPO_EINVAL, "%s: NULL argument", who);
-    if (n_rows < 0 || n_rows > (1 << 30) || max_new < 0 || max_new > n_rows)
-        return fail(RPO_EINVAL, "%s: need 0 <= max_new <= n_rows <= 2^30", who);
+    if (n_rows < 0 || n_rows > (1 << 30) || max_new < 0 || max_new > n_rows || max_new >= kMaxNew)
+        return fail(RPO_EINVAL, "%s: need 0 <= max_new <= n_rows <= 2^30, max_new < 2^26", who);
     return RPO_OK;
 }
 
@@ -1295,8 +1296,9 @@ int attn_args(const char* who, const rpo_paged_kv* kv, int n_rows, int max_new, 
     const int rc = paged_kv(who, kv, true, &a->kv);
     if (rc != RPO_OK) return rc;
     if (Hq < 1 || Hq > 65535 || Hq % a->kv.Hkv) return fail(RPO_EINVAL, "%s: n_q_heads must be a multiple of n_kv_heads, <= 65535", who);
-    if (n_rows < 0 || max_new < 0 || max_new > n_rows || n_rows > (1 << 30) || (int64_t)max_new * (Hq / a->kv.Hkv) > (1 << 30))
-        return fail(RPO_EINVAL, "%s: need 0 <= max_new <= n_rows, and n_rows and max_new * n_q_heads / n_kv_heads <= 2^30", who);
+    if (n_rows < 0 || max_new < 0 || max_new > n_rows || n_rows > (1 << 30) || max_new >= kMaxNew ||
+        (int64_t)max_new * (Hq / a->kv.Hkv) > (1 << 30))
+        return fail(RPO_EINVAL, "%s: need 0 <= max_new <= n_rows <= 2^30, max_new < 2^26, max_new * n_q_heads / n_kv_heads <= 2^30", who);
     if (max_len < 0) return fail(RPO_EINVAL, "%s: max_len must be >= 0", who);
     if (window < 0 || sinks < 0) return fail(RPO_EINVAL, "%s: window and n_sinks must be >= 0", who);
     const int64_t cap = (int64_t)a->kv.table_stride << a->kv.shift;
@@ -1304,7 +1306,7 @@ int attn_args(const char* who, const rpo_paged_kv* kv, int n_rows, int max_new, 
     a->max_new = max_new;
     a->max_len = (int)std::min((int64_t)max_len, cap);
     a->Hq = Hq;
-    a->window = window;
+    a->window = (int)std::min((int64_t)window, cap);  // a longer one hides nothing either
     a->sinks = window ? (int)std::min((int64_t)sinks, cap) : 0;
     a->q = nullptr;
     a->q_stride = a->out_stride = (int64_t)Hq * a->kv.dh;
