@@ -137,7 +137,14 @@ struct Span {
 __device__ inline uint32_t low_bits(int n) { return (uint32_t)((1ull << min(max(n, 0), 32)) - 1); }
 
 // ---------------------------------------------------------------------------
-// chunks
+// chunks.  A wave multiplies every fragment that it reads from LDS with two column tiles (32 columns), which takes the LDS to
+// half of the matrix units' time; 64 columns would need the registers of the second workgroup of a CU, whose waves fill each
+// other's gaps.  Direct loads leave the registers to the pipeline below; K is permuted on the way, V needs no permutation.
+// Bound by matrix and vector units about equally (products 1024 cycles, exponentials and their fma, sum and conversion 800
+// for a wave and a tile) and by what their taking turns leaves open: prefill of 4 x 4352 rows of 7B heads 545 us = 1.0 PFLOP/s,
+// where a large library product reaches 1.14.  One after the other in a tile 667 us; pipelined, fragments read just before
+// their products 613; read ahead 604; the maximum checked by lane and moved past 2^8 only 570; masks as bits, values
+// cleared in registers 545.
 // ---------------------------------------------------------------------------
 struct TileGeom {
     int combos;   // n_seqs * Hkv
@@ -489,7 +496,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
 }
 
 // ---------------------------------------------------------------------------
-// up to 16 query columns per KV head
+// up to 16 query columns per KV head.  The keys and values are used once, so they go to registers directly; a wave has the
+// next step's 16 KiB on their way while it multiplies.  Bound by memory: 128 sequences of 4250 tokens of 7B heads 197 us =
+// 5.7 TB/s (a large copy moves 4.8 TB/s both ways together); one token over 2176 7.9 us, four rounds of dependent loads.
 // ---------------------------------------------------------------------------
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileGeom geo) {
@@ -719,6 +728,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeo
 // ---------------------------------------------------------------------------
 // scores: the weights of a token summed over the query columns.  Products the other way round, S = Q K^T, so that a lane
 // holds scores of one token and its sum stays in one register; the keys of a wave's tokens stay in registers throughout.
+// Chunks are bound by vector and matrix units together (64 exponentials, fma and sums a lane and tile against 64 products):
+// 4 x 4352 rows of 7B heads 303 us = 0.9 PFLOP/s.  Single tokens by memory: 512 rows over 2100 tokens 113 us = 5.0 TB/s.
 // ---------------------------------------------------------------------------
 struct ScoreGeom {
     int combos;
@@ -835,7 +846,7 @@ __global__ __launch_bounds__(256) void score_few_kernel(PagedScoreArgs b, ScoreG
 }
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 3) void score_tile_kernel(PagedScoreArgs b, ScoreGeom geo) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void score_tile_kernel(PagedScoreArgs b, ScoreGeom geo) {
     using R = Row<T, DH>;
     using M = Mat<T>;
     constexpr int MB = kScoreBlocks<T>, QT = 64;      // query columns of a tile

@@ -535,3 +535,80 @@ def test_binding_refuses_what_does_not_fit():
             call()
         assert e.value.code == rpo.RPO_EINVAL
     assert torch.all(out == 0)
+
+
+@pytest.mark.parametrize("ties", [False, True])
+def test_evict_rows_too_long_for_registers(ties):
+    _evict_case([40000, 39000], 1, 32, 64, "bf16", 3000, 4, 100, seed=5, ties=ties)
+
+
+def test_calls_without_rows_and_without_tokens():
+    """No rows: attention does nothing, scores are copied; all caches empty: rows see nothing, nothing is kept."""
+    from paper_2601_19404_amd import binding as rpo
+    c = Cache([100, 30], 2, 128, 64, "bf16", seed=1)
+    q = torch.zeros(0, 12 * 128, dtype=torch.bfloat16, device="cuda")
+    cu = torch.zeros(3, dtype=torch.int32, device="cuda")
+    before = torch.rand(2, 2, 100).cuda()
+    after = torch.full_like(before, -1.0)
+    rpo.rpo_attn_paged(c.dev, q, cu, 0, torch.zeros_like(q))
+    rpo.rpo_kv_append(c.dev, q[:, :256], q[:, :256], cu, 0)
+    rpo.rpo_kv_score(c.dev, q, cu, 0, torch.zeros(0, 12, device="cuda"), before, after)
+    torch.cuda.synchronize()
+    for s, n in enumerate((100, 30)):
+        assert torch.equal(after[s, :, :n], before[s, :, :n]) and torch.all(after[s, :, n:] == -1)
+    rows, cu2, _ = _queries([2, 20], 12, 128, "bf16", seed=1)
+    c.dev.lens.zero_()
+    _check_attention(c, rows, cu2, [2, 20], 12, 0, 0, "bf16", True, lens=[0, 0], max_len=0)
+    to = Cache([0, 0], 2, 128, 64, "bf16", seed=2, cap=64, stale=3.0)
+    kept = torch.full((2, 2, 50), 5, dtype=torch.int32, device="cuda")
+    rpo.rpo_kv_evict(c.dev, before, 50, 0, 0, to.dev, to.dev.lens, kept)
+    assert to.dev.lens.tolist() == [0, 0] and torch.all(kept == -1) and torch.all(to.pool == 3)
+
+
+@pytest.mark.parametrize("layout", [LAYOUTS[0], LAYOUTS[1], LAYOUTS[10]], ids=lambda x: "-".join(map(str, x)))
+def test_the_largest_window_and_number_of_sinks(layout):
+    """2^31 - 1 of either hides nothing, also from rows far below slot 0."""
+    Hq, Hkv, dh, dtype, pt = layout
+    lens, news, most = [70, 3], [70, 40], 2 ** 31 - 1
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=4)
+    q, cu, _ = _queries(news, Hq, dh, dtype, seed=3)
+    for window, sinks in ((most, 0), (most, most), (5, most)):
+        lse, weights = _check_attention(c, q, cu, news, Hq, window, sinks, dtype, True)
+        _check_score(c, q, cu, news, Hq, window, sinks, lse, weights)
+
+
+@pytest.mark.parametrize("layout", [LAYOUTS[0], LAYOUTS[1], LAYOUTS[4]], ids=lambda x: "-".join(map(str, x)))
+@pytest.mark.parametrize("new", [1, 50])
+def test_scores_that_climb_by_hundreds(layout, new):
+    """Scores rise along the cache from far below to far above: the reference point of the weights has to move many times,
+    and weights that are due already move with it."""
+    Hq, Hkv, dh, dtype, pt = layout
+    lens, news = [330, 100], [new, min(new, 100)]
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=8)
+    pool = c.pool.cpu()
+    for s, n in enumerate(lens):
+        ramp = torch.linspace(-3.0, 3.0, n)[:, None, None] * torch.ones(1, Hkv, dh)
+        c.k[s] = (ramp + 0.05 * c.k[s].float()).to(c.k[s].dtype)
+        c.write(pool, s, torch.arange(n), c.k[s], c.v[s])
+    c.pool.copy_(pool)
+    q, cu, _ = _queries(news, Hq, dh, dtype, seed=3)
+    q = (q.float().abs() + 2.0).to(q.dtype)          # scores of about -100 (32 channels) to 250 (128)
+    for use_ws in (False, True):
+        lse, weights = _check_attention(c, q, cu, news, Hq, 0, 0, dtype, use_ws)
+        _check_score(c, q, cu, news, Hq, 0, 0, lse, weights)
+
+
+def test_a_nan_in_a_query_stays_in_its_row():
+    from paper_2601_19404_amd import binding as rpo
+    c = Cache([200], 2, 128, 64, "bf16", seed=4)
+    q, cu, _ = _queries([40], 12, 128, "bf16", seed=3)
+    q = q.clone()
+    want, lse = torch.zeros_like(q), torch.zeros(40, 12, device="cuda")
+    rpo.rpo_attn_paged(c.dev, q, cu, 40, want, lse_out_dev=lse)
+    q[7, 128:256] = float("nan")
+    out, lse2 = torch.zeros_like(q), torch.zeros(40, 12, device="cuda")
+    rpo.rpo_attn_paged(c.dev, q, cu, 40, out, lse_out_dev=lse2)
+    torch.cuda.synchronize()
+    assert out[7, 128:256].isnan().all() and lse2[7, 1].isnan()
+    out[7, 128:256], lse2[7, 1] = want[7, 128:256], lse[7, 1]
+    assert torch.equal(out, want) and torch.equal(lse, lse2)
