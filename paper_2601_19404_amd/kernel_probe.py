@@ -10,7 +10,10 @@ accumulate, 3 fused SwiGLU); `attn` fills the KV pages of a ONE-layer model of t
 with the C1 workload's prefixes (64 groups x 8 rollouts, ~2000-token shared prefixes) plus 100
 private tokens per rollout (written by a teacher-forced pass), then runs the shared-prefix decode
 attention alone five times
-(rpo_attn_decode; the dispatches named attn_decode_mfma_kernel are the ones to read).
+(rpo_attn_decode; the dispatches named attn_decode_mfma_kernel are the ones to read);
+`paged HQ,HKV,SEQS,LEN,NEW,WINDOW` runs the paged-cache operators five times each on SEQS caches of LEN
+tokens (128 channels, bf16, 64-token pages in random order): append of the last NEW rows, their
+attention (WINDOW 0: none, else with four sinks), the scores and an eviction to half of the tokens.
 Prints one JSON line naming what ran, with the algorithmic bytes of one launch where it applies.
 """
 from __future__ import annotations
@@ -80,8 +83,34 @@ def probe_attn(n_fill: int = 100, reps: int = 5) -> dict:
                                                   + sum(-(-((n % 64) + n_fill) // 64) for n in lens) * G) * 64 * kv_tok}
 
 
+def probe_paged(Hq: int, Hkv: int, seqs: int, length: int, new: int, window: int, reps: int = 5) -> dict:
+    pages, dt, dev = -(-length // 64), torch.bfloat16, "cuda"
+    pool, lens = torch.randn(seqs * pages, 2 * Hkv * 64 * 128, device=dev, dtype=dt), torch.full((seqs,), length, dtype=torch.int32, device=dev)
+    table = torch.randperm(seqs * pages, device=dev).to(torch.int32).view(seqs, pages)
+    kv = rpo.PagedKV(pool, table, lens, 64, Hkv, 128)
+    half = max(length // 2, 1)
+    to_pages = -(-half // 64)
+    to = rpo.PagedKV(torch.zeros(seqs * to_pages, pool.shape[1], device=dev, dtype=dt),
+                     torch.arange(seqs * to_pages, device=dev, dtype=torch.int32).view(seqs, to_pages), torch.zeros_like(lens), 64, Hkv, 128)
+    rows = seqs * new
+    q, k, v = (torch.randn(rows, h * 128, device=dev, dtype=dt) for h in (Hq, Hkv, Hkv))
+    cu = torch.arange(0, rows + 1, new, device=dev, dtype=torch.int32)
+    out, lse = torch.empty_like(q), torch.empty(rows, Hq, device=dev)
+    score, kept = torch.zeros(seqs, Hkv, length, device=dev), torch.empty(seqs, Hkv, half, dtype=torch.int32, device=dev)
+    sinks = 4 if window else 0
+    need = max(f(kv, rows, new, length, Hq, window, sinks) for f in (rpo.rpo_attn_paged_ws_bytes, rpo.rpo_kv_score_ws_bytes))
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    for _ in range(reps):
+        rpo.rpo_kv_append(kv, k, v, cu, new)
+        rpo.rpo_attn_paged(kv, q, cu, new, out, window, sinks, lse_out_dev=lse, ws_dev=ws, max_len=length)
+        rpo.rpo_kv_score(kv, q, cu, new, lse, None, score, window, sinks, ws_dev=ws, max_len=length)
+        rpo.rpo_kv_evict(kv, score, half, min(4, half), 0, to, to.lens, kept)
+    torch.cuda.synchronize()
+    return {"paged_probe": [Hq, Hkv, seqs, length, new, window], "launches": reps}
+
+
 def main(argv) -> int:
-    if len(argv) < 1 or argv[0] not in ("copy", "gemm", "attn") or (argv[0] == "gemm" and len(argv) != 2):
+    if len(argv) < 1 or argv[0] not in ("copy", "gemm", "attn", "paged") or (argv[0] in ("gemm", "paged") and len(argv) != 2):
         print(__doc__, file=sys.stderr)
         return 2
     if not torch.cuda.is_available():
@@ -92,6 +121,8 @@ def main(argv) -> int:
         out = probe_copy()
     elif argv[0] == "attn":
         out = probe_attn()
+    elif argv[0] == "paged":
+        out = probe_paged(*(int(v) for v in argv[1].split(",")))
     else:
         out = probe_gemm(*(int(v) for v in argv[1].split(",")))
     print(json.dumps(out), flush=True)
