@@ -109,12 +109,16 @@ __device__ inline int wave_min_int(int v) {
     return __builtin_amdgcn_readfirstlane(v);
 }
 __device__ inline int wave_max_int(int v) { return -wave_min_int(-v); }
-// the same address in every lane, in scalar registers
+// The same address in every lane, in scalar registers, for a load written as assembly: scalar registers that a vector
+// instruction has written may be read by a memory instruction five wait states later, which the compiler sees to only where
+// it knows the instruction.
 template <typename T>
 __device__ inline const T* uniform(const T* p) {
-    const uint64_t u = (uint64_t)(uintptr_t)p;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
-    return (const T*)(uintptr_t)((uint64_t)hi << 32 | lo);
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    uint64_t u = (uint64_t)hi << 32 | lo;
+    asm volatile("s_nop 4" : "+s"(u));
+    return (const T*)(uintptr_t)u;
 }
 
 // The slots that a set of rows sees any of, in steps of `step` tokens: [0, sink) and then [lo, hi), cut into pieces.

@@ -612,3 +612,93 @@ def test_a_nan_in_a_query_stays_in_its_row():
     assert out[7, 128:256].isnan().all() and lse2[7, 1].isnan()
     out[7, 128:256], lse2[7, 1] = want[7, 128:256], lse[7, 1]
     assert torch.equal(out, want) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("layout", [LAYOUTS[0], LAYOUTS[1], LAYOUTS[3]], ids=lambda x: "-".join(map(str, x)))
+def test_rows_off_16_bytes_and_the_generic_kernels(layout):
+    """Query rows that start anywhere take the generic kernels, as everything does with kernel path 1."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = layout
+    lens, news, window, sinks = [150, 70], [37, 3], 40, 3
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=4)
+    wide, cu, _ = _queries(news, Hq, dh, dtype, seed=3, extra=7)
+    off = torch.cat([wide[:, :1], wide], dim=1)[:, 1:]
+    assert off.data_ptr() % 16 and off.stride(0) * off.element_size() % 16
+    for q, path in ((off, 0), (wide.contiguous(), 1)):
+        rpo.rpo_set_kernel_path(path)
+        try:
+            lse, weights = _check_attention(c, q, cu, news, Hq, window, sinks, dtype, True)
+            _check_score(c, q, cu, news, Hq, window, sinks, lse, weights, True)
+        finally:
+            rpo.rpo_set_kernel_path(0)
+
+
+def test_two_calls_at_once_with_a_workspace_each():
+    from paper_2601_19404_amd import binding as rpo
+    streams, work, want = [torch.cuda.Stream() for _ in range(2)], [], []
+    for i in range(2):
+        c = Cache([3000, 1700], 2, 128, 64, "bf16", seed=i)
+        q, cu, _ = _queries([2, 2], 12, 128, "bf16", seed=i)
+        need = rpo.rpo_attn_paged_ws_bytes(c.dev, 4, 2, 3000, 12)
+        assert need > 0
+        work.append((c, q, cu, torch.zeros_like(q), torch.empty(need, dtype=torch.uint8, device="cuda")))
+    for c, q, cu, out, ws in work:
+        rpo.rpo_attn_paged(c.dev, q, cu, 2, out, ws_dev=ws, max_len=3000)
+    torch.cuda.synchronize()
+    want = [w[3].clone() for w in work]
+    for w in work:
+        w[3].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (c, q, cu, out, ws), s in zip(work, streams):
+            rpo.rpo_attn_paged(c.dev, q, cu, 2, out, ws_dev=ws, max_len=3000, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(w[3], x) for w, x in zip(work, want))
+
+
+def test_a_batchs_cache_is_scored_and_evicted_into_pages_of_ones_own():
+    """Prefill and fork a batch, score its prefix with queries of one's own, keep half of every rollout's cache and attend to
+    what is left: the oracle's attention over the kept tokens of the batch's pages."""
+    from paper_2601_19404_amd import binding as rpo
+    from paper_2601_19404_amd import synth
+    from tests.util import to_device
+    mc = synth.ModelCfg("1.5B-heads", 1, 256, 12, 2, 128, 512, 1000, "bf16")
+    model = rpo.rpo_model_create(mc, to_device(synth.make_weights(mc)))
+    n_groups, G, plen = 2, 2, [150, 201]
+    batch = rpo.rpo_batch_create(model, n_groups, G, 256, 32, 64, 512)
+    g = torch.Generator().manual_seed(0)
+    toks = torch.randint(0, 1000, (sum(plen),), generator=g, dtype=torch.int32).cuda()
+    rpo.rpo_prefill_prefix(batch, toks, [0, 150, 351], torch.zeros(n_groups, 1000, device="cuda"))
+    rpo.rpo_kv_fork(batch)
+    lens = [plen[r // G] for r in range(4)]
+    kv = rpo.PagedKV.of_batch(batch, 0, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    q, cu, _ = _queries([3] * 4, 12, 128, "bf16", seed=3)
+    out, lse = torch.zeros_like(q), torch.zeros(12, 12, device="cuda")
+    score = torch.zeros(4, 2, 201, device="cuda")
+    pool_before = batch.kv_pool.clone()
+    rpo.rpo_attn_paged(kv, q, cu, 3, out, lse_out_dev=lse)
+    rpo.rpo_kv_score(kv, q, cu, 3, lse, None, score)
+    budget = 90
+    to = Cache([0] * 4, 2, 128, 64, "bf16", seed=2, cap=budget, stale=float("nan"))
+    kept = torch.zeros(4, 2, budget, dtype=torch.int32, device="cuda")
+    rpo.rpo_kv_evict(kv, score, budget, 4, 16, to.dev, to.dev.lens, kept)
+    rpo.rpo_attn_paged(to.dev, q, cu, 3, out, lse_out_dev=lse)
+    torch.cuda.synchronize()
+    assert torch.equal(batch.kv_pool, pool_before) and to.dev.lens.tolist() == [budget] * 4
+    w = score.cpu().numpy()
+    assert np.allclose(w.sum(axis=(1, 2)), 3 * 12, rtol=1e-4)          # every row gives each of its heads' weights once
+    pool = batch.kv_pool.view(torch.bfloat16).view(-1, 2, 2, 64 * 128).cpu()     # one layer
+    pages = lambda r: [(r // G) * 4 + k if k < plen[r // G] // 64 else 2 * 4 + r * batch_private for k in range(-(-lens[r] // 64))]  # noqa: E731
+    batch_private = -(-(64 - 1 + 32) // 64)
+    got = out.float().cpu().numpy().reshape(4, 3, 12, 128)
+    for r in range(4):
+        K = torch.cat([pool[p, 0].view(2, 64, 128) for p in pages(r)], dim=1)
+        V = torch.cat([pool[p, 1].view(2, 8, 128, 8).permute(0, 1, 3, 2).reshape(2, 64, 128) for p in pages(r)], dim=1)
+        for h in range(2):
+            slots = kept[r, h].tolist()
+            assert slots == O.evict(w[r, h, : lens[r]].astype(np.float64), budget, 4, 16)
+            keys, values = to.read(r, list(range(budget)), h)
+            assert torch.equal(keys, K[h, slots]) and torch.equal(values, V[h, slots])
+            rows = q[3 * r: 3 * r + 3].float().cpu().numpy().reshape(3, 2, 6, 128)[:, h]
+            ref, _, p, mag, big = O.attention(rows, K[h, slots].float().numpy()[:, None], V[h, slots].float().numpy()[:, None], 128 ** -0.5)
+            assert np.all(np.abs(got[r][:, 6 * h: 6 * h + 6] - ref) <= _tolerance(budget, 128, ref, mag, big, "bf16"))
