@@ -135,6 +135,7 @@ struct Span {
     }
     __device__ int step_at(int i) const { return i < sink_steps ? i : lo_step + i - sink_steps; }
     __device__ bool any(int j) const { return j < hi && (j < sinks || j >= lo); }
+    __device__ bool any_of(int j, int n) const { return j < hi && (j < sinks || j + n > lo); }  // any of n slots
 };
 
 // the lowest n bits (n below 0: none, above 32: all)
@@ -542,22 +543,33 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
         const int slot = span.step_at(it) * KS + 16 * u;
         return it < it1 && slot < span.hi ? kv.page(s, slot) : -1;
     };
-    u32x4_t ak[2][MB][R::kFrags], av[2][DH / 16];
+    u32x4_t ak[2][MB][R::kFrags] = {}, av[2][DH / 16] = {};
+    constexpr int kTok = M::kLaneTok;  // tokens of a lane's values; its keys are of the same many at most
     auto load = [&](int it, int pk, int pv, u32x4_t (&k)[MB][R::kFrags], u32x4_t (&v)[DH / 16]) {
         const int tok0 = span.step_at(it) * KS;
-        // a page that is not there: page 0 is read in its place, and masked
+        // What is not there or not seen is not read (it is masked); at the edges of a window and of the sinks that counts:
+        // 512 tokens and 4 sinks lie in 18 steps of 32 (512 rows of 1.5B heads 62.9 us with whole steps, 60.4 without).
+        bool want_k = pk >= 0, want_v = pv >= 0;
+        if (tok0 + KS > span.hi || (tok0 < span.lo && tok0 + KS > span.sinks)) {
+            want_k = want_k && span.any_of(tok0 + key_tok / kTok * kTok, kTok);
+            want_v = want_v && span.any_of(tok0 + kTok * g, kTok);
+        }
         const T* kp = pool + kv.k_at(max(pk, 0), kh) + (int64_t)((tok0 + key_tok) & mask) * DH + g * R::kElems;
         const T* vp = pool + kv.k_at(max(pv, 0), kh) + to_values + (int64_t)((tok0 + 16 * val_unit) & mask) * DH;
         // units of values from there: as M::unit counts them, less the 16-token units before
         const int u0 = M::unit(0, g, DH, c16) - val_unit * 2 * DH;
+        if (want_k) {
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
+            for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-            for (int j = 0; j < R::kFrags; ++j)
-                k[mb][j] = *(const u32x4_t*)(kp + (M::token(mb, 0) - M::token(0, 0)) * DH + 4 * j * R::kElems);
+                for (int j = 0; j < R::kFrags; ++j)
+                    k[mb][j] = *(const u32x4_t*)(kp + (M::token(mb, 0) - M::token(0, 0)) * DH + 4 * j * R::kElems);
+        }
+        if (want_v) {
 #pragma unroll
-        for (int i = 0; i < DH / 16; ++i)
-            v[i] = *(const u32x4_t*)(vp + (int64_t)(u0 + (sizeof(T) == 2 ? 16 : 32) * i) * R::kElems);
+            for (int i = 0; i < DH / 16; ++i)
+                v[i] = *(const u32x4_t*)(vp + (int64_t)(u0 + (sizeof(T) == 2 ? 16 : 32) * i) * R::kElems);
+        }
     };
     f32x4_t ot[DH / 16];
 #pragma unroll
@@ -587,7 +599,6 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
                     sc[mb][i] = seen ? sc[mb][i] : -INFINITY;
                 }
             // values that no row sees may be anything
-            constexpr int kTok = sizeof(T) == 2 ? 8 : 4;
             const int first = tok0 + kTok * g;
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) {
