@@ -87,9 +87,9 @@ typedef struct {
 int rpo_batch_kv(const struct rpo_batch *b, int32_t layer, rpo_paged_kv *out);
 
 /* The rows of a call (below): sequence s has rows cu_rows_dev[s] .. cu_rows_dev[s + 1] - 1 of the row arrays, any number from
- * 0 up to max_new (the longest, below 2^26; a host bound that sizes the launch: rows of a sequence beyond it are not looked at).  They
- * are the last tokens of its cache: with n rows, row i sits at slot len - n + i.  cu_rows_dev: device int32 [n_seqs + 1],
- * not decreasing.  Rows of the arrays that belong to no sequence are left as they were.
+ * 0 up to max_new (the longest, below 2^26; a host bound that sizes the launch: rows of a sequence beyond it are not looked
+ * at).  They are the last tokens of its cache: with n rows, row i sits at slot len - n + i.  cu_rows_dev: device int32
+ * [n_seqs + 1], not decreasing.  Rows of the arrays that belong to no sequence are left as they were.
  *
  * rpo_kv_append: write the rows' keys and values into their slots (len_dev counts them already).
  *   k_dev, v_dev  device, n_rows rows of n_kv_heads * head_dim values, k_stride / v_stride elements apart
@@ -147,7 +147,7 @@ int rpo_kv_score(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, co
  *   score_out_dev device fp32 [n_seqs, n_kv_heads, score_out_stride] or NULL, score_out_stride >= budget, not score_dev: the
  *                 kept tokens' scores, 0 in the rest of the row
  *   kept_out_dev  device int32 [n_seqs, n_kv_heads, budget]: the old slot of every new one, -1 beyond the length
- * Errors: RPO_EINVAL, RPO_EHIP. */
+ * A kept token whose page is not there leaves its new slot as it was.  Errors: RPO_EINVAL, RPO_EHIP. */
 int rpo_kv_evict(const rpo_paged_kv *src, const float *score_dev, int64_t score_stride, int32_t budget, int32_t n_sinks,
                  int32_t n_recent, const rpo_paged_kv *dst, int32_t *len_out_dev, float *score_out_dev,
                  int64_t score_out_stride, int32_t *kept_out_dev, void *stream);

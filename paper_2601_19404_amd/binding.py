@@ -457,8 +457,8 @@ class PagedKV:
         return self
 
 
-# A decode step makes these calls layer by layer: their checks are kept to a few attribute reads (8 us of a call's 13 before
-# went into them, 4 now).
+# A decode step makes these calls layer by layer: their checks are kept to a few attribute reads (2.9 us of a call, of which
+# 1.3 are ctypes; 3.4 more are the launch).
 def _on(kv: PagedKV, stream, *tensors) -> int:
     """The stream to launch on; the cache has to lie on the current device, and every tensor and the stream there too."""
     index = kv.index
