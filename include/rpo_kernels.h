@@ -110,7 +110,8 @@ int rpo_kv_append(const rpo_paged_kv *kv, const void *k_dev, int64_t k_stride, c
  *               that may run at the same time (captured graphs among them) need one each.
  * bf16 and fp32 with head_dim 32, 64 or 128 and rows that start at multiples of 16 bytes run on the matrix cores, anything
  * else on a generic kernel.  Sums and statistics are fp32; with bf16 the weights p are rounded to bf16 before they multiply
- * the values, as in the batch's attention.  A NaN or infinity in a slot reaches the rows that see it and may reach the rows
+ * the values, as in the batch's attention, and those of a chunk are divided by their sum as rounded, so that equal values come
+ * out as they are.  A NaN or infinity in a slot reaches the rows that see it and may reach the rows
  * of the same sequence that are computed together with them; in slots that no row of the call sees it does nothing.
  * Errors: RPO_EINVAL, RPO_ENOMEM (ws_bytes), RPO_EHIP. */
 size_t rpo_attn_paged_ws_bytes(const rpo_paged_kv *kv, int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads,

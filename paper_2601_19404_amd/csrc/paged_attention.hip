@@ -17,6 +17,8 @@
 // 16x16x4 fp32 instructions multiply.  Scores are computed transposed, S^T = K Q^T, so that a lane holds scores of one query
 // column and its maximum and sum need two lane swaps; and the rows of K are dealt to the instruction such that the weights a
 // lane ends with are eight (four) consecutive tokens, which is how a page keeps the values: they are read as they lie.
+#include <type_traits>
+
 #include "kernels.hpp"
 
 namespace rpo {
@@ -146,18 +148,33 @@ __device__ inline uint32_t low_bits(int n) { return (uint32_t)((1ull << min(max(
 // half of the matrix units' time; 64 columns would need the registers of the second workgroup of a CU, whose waves fill each
 // other's gaps.  Direct loads leave the registers to the pipeline below; K is permuted on the way, V needs no permutation.
 // Bound by matrix and vector units about equally (products 1024 cycles, exponentials and their fma, sum and conversion 800
-// for a wave and a tile) and by what their taking turns leaves open: prefill of 4 x 4352 rows of 7B heads 545 us = 1.0 PFLOP/s,
-// where a large library product reaches 1.14.  One after the other in a tile 667 us; pipelined, fragments read just before
+// for a wave and a tile) and by what their taking turns leaves open: prefill of 4 x 4352 rows of 7B heads 542 us = 1.0 PFLOP/s,
+// with the log-sum-exp 564, where a large library product reaches 1.14.  One after the other in a tile 667 us; pipelined, fragments read just before
 // their products 613; read ahead 604; the maximum checked by lane and moved past 2^8 only 570; masks as bits, values
 // cleared in registers 545.
+// Weights are rounded to bf16 before they meet the values, which takes the matrix units' full rate; the output is divided by
+// the sum of the weights as they were rounded, so that it is a mean of the values with weights a little off and a row that sees
+// equal values (or one) returns them.  Divided by the unrounded sum it is off by the largest weight's rounding too: 1.4e-3
+// instead of 0 for rows that see one token, 2.3e-3 instead of 2.15e-3 over 512 to 4352 tokens, the result's own rounding 1.7e-3
+// among it.  That sum comes from a product with ones (as a sum of converted weights: 588 us, with the log-sum-exp), the
+// unrounded one, which the log-sum-exp needs, is added up only where it is asked for.
 // ---------------------------------------------------------------------------
 struct TileGeom {
     int combos;   // n_seqs * Hkv
     int n_split;  // pieces that the tokens are cut into
-    float* part;  // n_split > 1: [row, head, piece][DH] sums, then [row, head, piece][2] maximum (log2 domain) and sum
+    float* part;  // n_split > 1: [row, head, piece][DH] sums, then [row, head, piece] PieceSums
 };
+// Of a piece's weights: what they are relative to (log2 domain; -infinity if nothing is seen), the sum that divides the output, the
+// sum that the log-sum-exp is made of.
+struct alignas(16) PieceSums {
+    float top, sum, lse_sum, unused;
+};
+template <int DH>
+__device__ inline PieceSums* piece_sums(const PagedAttnArgs& a, const TileGeom& geo) {
+    return (PieceSums*)(geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH);
+}
 
-template <typename T, int DH, int NC, bool WIDE>
+template <typename T, int DH, int NC, bool WIDE, bool LSE>
 __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, TileGeom geo) {
     using R = Row<T, DH>;
     using M = Mat<T>;
@@ -206,7 +223,10 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
     f32x4_t ot[NC][DH / 16];
     // weights are 2^(scale_log2 score + minus_ref), minus_ref a whole number; it moves when a score passes bound (-infinity
     // before the first one)
-    float minus_ref[NC], bound[NC], l[NC];
+    float minus_ref[NC], bound[NC], l[NC];  // l: a lane's share of the sum of the weights before they are rounded
+    f32x4_t lr[NC];                         // every element: the sum of a column's weights as they are multiplied (bf16)
+    constexpr bool kRounds = sizeof(T) == 2;
+    static_assert(LSE || kRounds, "without roundings there is one sum");
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -214,6 +234,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         minus_ref[c] = 0.f;
         bound[c] = -INFINITY;
         l[c] = 0.f;
+        lr[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
@@ -303,6 +324,11 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
             for (int c = 0; c < NC; ++c) ot[c][i] = M::mma(vf[i], p[c], ot[c][i]);
+        if constexpr (kRounds) {
+            constexpr uint32_t kOnes = 0x3f803f80u;  // two of bf16
+#pragma unroll
+            for (int c = 0; c < NC; ++c) lr[c] = M::mma(u32x4_t{kOnes, kOnes, kOnes, kOnes}, p[c], lr[c]);
+        }
     };
     auto gone_mask = [&](int gone) -> uint32_t {  // bit r: token r of a half tile is not there
         return WIDE ? (gone ? ~0u : 0u) : (gone & 1 ? 0xffffu : 0u) | (gone & 2 ? 0xffff0000u : 0u);
@@ -361,6 +387,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
             minus_ref[c] = -next;
             bound[c] = move ? (next + 8.f) * inv_scale : bound[c];
             l[c] *= down;
+            lr[c][0] *= down;
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) ot[c][i] *= down;
             due[c] = M::times(due[c], down);
@@ -375,7 +402,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
                 for (int i = 0; i < 4; ++i) {
                     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][mb][i], scale_log2, minus_ref[c]));
                     sc[c][mb][i] = w;
-                    l[c] += w;
+                    if constexpr (LSE) l[c] += w;
                 }
             p[c] = M::weights(sc[c]);
         }
@@ -476,7 +503,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const float total = sum_over_lane_groups(l[c]);
+        const float total = LSE ? sum_over_lane_groups(l[c]) : lr[c][0];
+        const float sum = kRounds ? lr[c][0] : total;
         int col = qt * kCols + (wave * NC + c) * 16 + c16;
         asm volatile("" : "+v"(col));  // worked out again rather than kept in registers for the whole loop
         if (col >= n_cols) continue;
@@ -484,19 +512,18 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         const int head = kh * hpk + col % hpk;
         if (geo.n_split > 1) {
             const int64_t piece = (row * a.Hq + head) * geo.n_split + split;
-            float* ml = geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH + 2 * piece;
-            if (g == 0) ml[0] = total != 0.f ? -minus_ref[c] : -INFINITY, ml[1] = total;
+            if (g == 0) piece_sums<DH>(a, geo)[piece] = {sum != 0.f ? -minus_ref[c] : -INFINITY, sum, total, 0.f};
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)(geo.part + piece * DH + 16 * i + 4 * g) = ot[c][i];
             continue;
         }
-        const float inv = total != 0.f ? 1.0f / total : 0.f;
+        const float inv = sum != 0.f ? 1.0f / sum : 0.f;
         T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH;
 #pragma unroll
         for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[16 * i + 4 * g + e] = from_f32<T>(ot[c][i][e] * inv);
-        if (a.lse && g == 0) a.lse[row * a.Hq + head] = total != 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total) : -INFINITY;
+        if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum != 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total) : -INFINITY;
     }
 }
 
@@ -679,8 +706,7 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
         if (geo.n_split > 1) {
             const int64_t piece = at * geo.n_split + split;
             *(f32x4_t*)(geo.part + piece * DH + ch) = o;
-            float* ml = geo.part + (int64_t)a.n_rows * a.Hq * geo.n_split * DH + 2 * piece;
-            if (ch == 0) ml[0] = top, ml[1] = total;
+            if (ch == 0) piece_sums<DH>(a, geo)[piece] = {top, total, total, 0.f};
             continue;
         }
         const float inv = total != 0.f ? 1.0f / total : 0.f;
@@ -702,34 +728,36 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeo
     if (i >= cr.n) return;
     const int head = (int)(x % per_row) / (DH / 4), ch = (int)(x % (DH / 4)) * 4;
     const int64_t row = cr.row0 + i, at = row * a.Hq + head, piece = at * n_split;
-    const float* ml = geo.part + (int64_t)a.n_rows * a.Hq * n_split * DH + 2 * piece;
+    const PieceSums* sums = piece_sums<DH>(a, geo) + piece;
     const float* po = geo.part + piece * DH + ch;
     // eight pieces' loads at once: what counts is the number of times that memory is waited for
     constexpr int kAtOnce = 8;
-    float top = -INFINITY, total = 0.f;
+    float top = -INFINITY, total = 0.f, lse_total = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
     for (int p0 = 0; p0 < n_split; p0 += kAtOnce) {
-        float m[kAtOnce], l[kAtOnce];
+        PieceSums of[kAtOnce];
         f32x4_t v[kAtOnce];
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
             const int p = min(p0 + y, n_split - 1);
-            m[y] = ml[2 * p], l[y] = ml[2 * p + 1];
+            of[y] = sums[p];
             v[y] = *(const f32x4_t*)(po + (int64_t)p * DH);
         }
         float next = top;
 #pragma unroll
-        for (int y = 0; y < kAtOnce; ++y) next = fmaxf(next, m[y]);
+        for (int y = 0; y < kAtOnce; ++y) next = fmaxf(next, of[y].top);
         if (next == -INFINITY) continue;  // nothing seen so far
         const float down = __builtin_amdgcn_exp2f(top - next);
         top = next;
         total *= down;
+        lse_total *= down;
         o *= down;
 #pragma unroll
         for (int y = 0; y < kAtOnce; ++y) {
-            if (p0 + y >= n_split || m[y] == -INFINITY) continue;  // a piece that saw nothing holds anything
-            const float wgt = __builtin_amdgcn_exp2f(m[y] - top);
-            total += wgt * l[y];
+            if (p0 + y >= n_split || of[y].top == -INFINITY) continue;  // a piece that saw nothing holds anything
+            const float wgt = __builtin_amdgcn_exp2f(of[y].top - top);
+            total += wgt * of[y].sum;
+            lse_total += wgt * of[y].lse_sum;
             o += wgt * v[y];
         }
     }
@@ -737,7 +765,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeo
     T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH + ch;
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] = from_f32<T>(o[e] * inv);
-    if (a.lse && ch == 0) a.lse[at] = total != 0.f ? top * (1.0f / kLog2e) + logf(total) : -INFINITY;
+    if (a.lse && ch == 0) a.lse[at] = total != 0.f ? top * (1.0f / kLog2e) + logf(lse_total) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -1142,9 +1170,13 @@ hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
     const int64_t join = ceil_div64((int64_t)a.max_new * a.Hq * (DH / 4), 256);
     if (grid > kMaxGrid || join > kMaxGrid) return hipErrorInvalidValue;
     const bool wide = (1 << a.kv.shift) >= 2 * Mat<T>::kGroup, small = tile_cols(a) == 64;
+    auto tiles = [&](auto lse) {
+        return wide ? (small ? attn_tile_kernel<T, DH, 1, true, lse.value> : attn_tile_kernel<T, DH, 2, true, lse.value>)
+                    : (small ? attn_tile_kernel<T, DH, 1, false, lse.value> : attn_tile_kernel<T, DH, 2, false, lse.value>);
+    };
     auto kernel = few_take(a) ? attn_few_kernel<T, DH>
-                  : wide      ? (small ? attn_tile_kernel<T, DH, 1, true> : attn_tile_kernel<T, DH, 2, true>)
-                              : (small ? attn_tile_kernel<T, DH, 1, false> : attn_tile_kernel<T, DH, 2, false>);
+                  : a.lse     ? tiles(std::true_type{})
+                              : tiles(std::bool_constant<sizeof(T) == 4>{});  // fp32 has one sum for both
     kernel<<<(unsigned)grid, 256, 0, s>>>(a, geo);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || geo.n_split == 1) return e;
@@ -1194,7 +1226,7 @@ hipError_t launch_score_tiles(const PagedScoreArgs& b, hipStream_t s) {
 
 size_t paged_attn_ws_bytes(const PagedAttnArgs& a) {
     const int n = attn_splits(a);
-    return n == 1 ? 0 : (size_t)a.n_rows * a.Hq * n * (a.kv.dh + 2) * 4;
+    return n == 1 ? 0 : (size_t)a.n_rows * a.Hq * n * (a.kv.dh * 4 + sizeof(PieceSums));
 }
 size_t paged_score_ws_bytes(const PagedScoreArgs& b) {
     const int n = score_splits(b);
