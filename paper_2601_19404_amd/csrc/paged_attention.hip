@@ -706,7 +706,10 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
         if (geo.n_split > 1) {
             const int64_t piece = at * geo.n_split + split;
             *(f32x4_t*)(geo.part + piece * DH + ch) = o;
-            if (ch == 0) piece_sums<DH>(a, geo)[piece] = {top, total, total, 0.f};
+            // A piece is empty if its sum is 0.  Scores that are all NaN have no maximum (fmaxf passes them over), but their sum,
+            // a NaN, has to reach the join.
+            const float ref = total == 0.f ? -INFINITY : top == -INFINITY ? 0.f : top;
+            if (ch == 0) piece_sums<DH>(a, geo)[piece] = {ref, total, total, 0.f};
             continue;
         }
         const float inv = total != 0.f ? 1.0f / total : 0.f;

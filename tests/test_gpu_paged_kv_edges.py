@@ -59,3 +59,40 @@ def test_chunks_over_equal_values_return_the_value(layout, new, use_ws):
         else:
             off = (out.cpu() - want).abs() - (2 * max(lens) + 4) * EPS * want.abs()
             assert off.max() <= 0, (window, sinks, off.max())
+
+
+# new 1: the kernel for few rows, 40: the one for chunks; both are split over the tokens if there is a workspace
+@pytest.mark.parametrize("layout", [TINY, B128, B64, F128], ids=ids)
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("use_ws", [False, True])
+def test_a_nan_in_a_query_head_is_seen_in_it_alone(layout, new, use_ws):
+    Hq, Hkv, dh, dtype, pt = layout
+    c = Cache([2176, 257], Hkv, dh, pt, dtype, seed=2)
+    q, cu, _ = _queries([new, new], Hq, dh, dtype, seed=3)
+    q = q.clone()
+    want, want_lse = _attend(c, q, cu, new, Hq, use_ws=use_ws, must_split=True)
+    row, head = 2 * new - 1, Hq - 1
+    q[row, head * dh + 1] = float("nan")
+    out, lse = _attend(c, q, cu, new, Hq, use_ws=use_ws)
+    assert out[row, head * dh:].isnan().all() and lse[row, head].isnan()
+    out[row, head * dh:], lse[row, head] = want[row, head * dh:], want_lse[row, head]
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("layout", [TINY, B128, B64, F128], ids=ids)
+@pytest.mark.parametrize("slot", [256, 255, 100, 0])
+@pytest.mark.parametrize("use_ws", [False, True])
+def test_a_nan_in_a_key_reaches_the_single_token_that_sees_it(layout, slot, use_ws):
+    """Slot 256 of 257 is the only token of its piece: the newest one."""
+    Hq, Hkv, dh, dtype, pt = layout
+    c = Cache([2176, 257], Hkv, dh, pt, dtype, seed=2)
+    q, cu, _ = _queries([1, 1], Hq, dh, dtype, seed=3)
+    want, want_lse = _attend(c, q, cu, 1, Hq, use_ws=use_ws, must_split=True)
+    bad = c.k[1][slot:slot + 1].clone()
+    bad[:, Hkv - 1, dh - 1] = float("nan")
+    _rewrite(c, 1, [slot], k=bad)
+    out, lse = _attend(c, q, cu, 1, Hq, use_ws=use_ws)
+    first = (Hkv - 1) * (Hq // Hkv)                    # of the heads that read the last KV head
+    assert out[1, first * dh:].isnan().all() and lse[1, first:].isnan().all()
+    assert torch.equal(out[0], want[0]) and torch.equal(lse[0], want_lse[0])
+    assert torch.equal(out[1, : first * dh], want[1, : first * dh]) and torch.equal(lse[1, :first], want_lse[1, :first])
