@@ -71,8 +71,9 @@ int rpo_attn_decode(struct rpo_batch *b, int32_t layer, const void *q_dev, int32
  *   len_dev       device int32 [n_seqs]: slots in use.  What lies in other slots does not matter, NaN included
  *   n_seqs at most 65535; page_tokens a power of two, >= 16; head_dim even, <= 256; dtype RPO_F32 or RPO_BF16
  * What lies on the device cannot be checked on the host.  Every index from there is bounded by the kernels: a table entry
- * outside [0, n_pages) means that its tokens are not there (not visible, neither read nor written), a length counts up to
- * table_stride * page_tokens, row ranges end with the row arrays.  Several sequences may share pages that are only read. */
+ * outside [0, n_pages) means that its tokens are not there (not visible, neither read nor written), a length beyond
+ * table_stride * page_tokens is taken for that (by rpo_kv_append: as it is, the slots behind the table's end do not exist),
+ * row ranges end with the row arrays.  Several sequences may share pages that are only read. */
 typedef struct {
     void *pool_dev;
     const int32_t *table_dev;
@@ -93,7 +94,7 @@ int rpo_batch_kv(const struct rpo_batch *b, int32_t layer, rpo_paged_kv *out);
  *
  * rpo_kv_append: write the rows' keys and values into their slots (len_dev counts them already).
  *   k_dev, v_dev  device, n_rows rows of n_kv_heads * head_dim values, k_stride / v_stride elements apart
- * Rows that would lie below slot 0 or beyond the table are dropped.  Errors: RPO_EINVAL, RPO_EHIP. */
+ * Rows that would lie below slot 0 or beyond the table are dropped: a full cache stays as it is.  Errors: RPO_EINVAL, RPO_EHIP. */
 int rpo_kv_append(const rpo_paged_kv *kv, const void *k_dev, int64_t k_stride, const void *v_dev, int64_t v_stride,
                   const int32_t *cu_rows_dev, int32_t n_rows, int32_t max_new, void *stream);
 

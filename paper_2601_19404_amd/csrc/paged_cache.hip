@@ -28,8 +28,12 @@ template <typename T>
 __global__ __launch_bounds__(256) void append_kernel(PagedAppendArgs a, bool wide) {
     const PagedKv& kv = a.kv;
     const int s = blockIdx.y;
-    const ChunkRows c = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
-    const int from = max(c.slot0, 0), to = min(c.slot0 + c.n, kv.table_stride << kv.shift);  // slots written
+    // A row's slot counts from the length as it is given: beyond the table's end there is none.
+    ChunkRows c = chunk_rows(kv, a.cu, s, a.n_rows, a.max_new);
+    const int cap = kv.table_stride << kv.shift;
+    c.slot0 += max(kv.len[s], 0) - kv.length(s);
+    const int from = max(c.slot0, 0), to = min(c.slot0 + c.n, cap);  // slots written
+    if (from >= to) return;
     const int slot8 = ((from >> 3) + (int)blockIdx.x) * 8;                                    // an octet lies in one page
     const int lo = max(from, slot8), hi = min(to, slot8 + 8);
     if (lo >= hi) return;

@@ -96,3 +96,45 @@ def test_a_nan_in_a_key_reaches_the_single_token_that_sees_it(layout, slot, use_
     assert out[1, first * dh:].isnan().all() and lse[1, first:].isnan().all()
     assert torch.equal(out[0], want[0]) and torch.equal(lse[0], want_lse[0])
     assert torch.equal(out[1, : first * dh], want[1, : first * dh]) and torch.equal(lse[1, :first], want_lse[1, :first])
+
+
+@pytest.mark.parametrize("layout", [TINY, B128, B96], ids=ids)
+@pytest.mark.parametrize("over,news", [([1, 0, 3], [1, 1, 1]), ([5, 200, 2 ** 30], [9, 150, 20]),
+                                       ([0, 2 ** 31 - 1 - 128, 40], [128, 1, 40])])
+def test_append_drops_the_rows_behind_the_table(layout, over, news):
+    """Lengths past what the table holds (128 slots): rows behind its end are dropped, the others land in their slots, and
+    tokens that are there stay."""
+    from paper_2601_19404_amd import binding as rpo
+    _, Hkv, dh, dtype, pt = layout
+    S, cap = 3, 128
+    c = Cache([cap] * S, Hkv, dh, pt, dtype, seed=3, stale=5.0)
+    lens = [cap + x for x in over]
+    c.dev.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    rows = torch.randn(sum(news), 2, Hkv, dh, generator=torch.Generator().manual_seed(1)).to(c.pool.dtype)
+    want, row = c.pool.cpu().clone(), 0
+    for s in range(S):
+        slots = torch.arange(lens[s] - news[s], lens[s])
+        keep = (slots >= 0) & (slots < cap)
+        c.write(want, s, slots[keep], rows[row: row + news[s]][keep, 0], rows[row: row + news[s]][keep, 1])
+        row += news[s]
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(news)]), dtype=torch.int32).cuda()
+    flat = rows.cuda().view(sum(news), -1)
+    rpo.rpo_kv_append(c.dev, flat[:, : Hkv * dh], flat[:, Hkv * dh:], cu, max(news))
+    torch.cuda.synchronize()
+    assert torch.equal(c.pool.cpu(), want)
+
+
+def test_a_decode_loop_at_a_full_cache_leaves_it_alone():
+    """Rows that find no room are dropped, and attention goes on over the tokens that are there."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = B128
+    c = Cache([128], Hkv, dh, pt, dtype, seed=3)
+    before = c.pool.clone()
+    q, cu, _ = _queries([1], Hq, dh, dtype, seed=3)
+    want, want_lse = _attend(c, q, cu, 1, Hq)
+    for step in range(1, 4):
+        c.dev.lens.fill_(128 + step)
+        rpo.rpo_kv_append(c.dev, q[:, :256], q[:, 256:512], cu, 1)
+        out, lse = _attend(c, q, cu, 1, Hq)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert torch.equal(c.pool.view(torch.uint8), before.view(torch.uint8))
