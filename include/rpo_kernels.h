@@ -123,7 +123,8 @@ int rpo_attn_paged(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, 
 
 /* Attention weight that the cached tokens receive from the rows: for every slot j < len of every KV head
  *   score_out = score_in + sum over rows and the head's query heads that see j of exp(scale q k_j - lse)
- * lse_dev device fp32 [n_rows, n_q_heads]: what rpo_attn_paged left for the same rows (a row with -infinity gives nothing).
+ * lse_dev device fp32 [n_rows, n_q_heads]: what rpo_attn_paged left for the same rows (a row with -infinity gives nothing,
+ * whatever its query holds).
  *   score_in_dev  device fp32 [n_seqs, n_kv_heads, score_stride] or NULL: zeros; score_out_dev the same layout, may be the
  *                 same array.  score_stride >= the longest cache (slots beyond it get no score); slots from len on are left
  *                 as they were.  The sums run in a fixed order: equal inputs give equal bits.

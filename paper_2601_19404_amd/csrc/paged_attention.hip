@@ -865,13 +865,14 @@ __global__ __launch_bounds__(256) void score_few_kernel(PagedScoreArgs b, ScoreG
 #pragma unroll
         for (int j = 0; j < R::kFrags; ++j) q[j] = *(const u32x4_t*)(qp + (4 * j + g) * R::kElems);
         int t[4];
-        float shift[4];  // -lse in the log2 domain; what gives nothing is infinitely far down
+        float shift[4];  // -lse in the log2 domain
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int x = 4 * g + i, y = x < n_cols ? x : 0;
             const float lse = b.lse_in[(int64_t)(cr.row0 + y / hpk) * a.Hq + kh * hpk + y % hpk];
-            t[i] = cr.slot0 + y / hpk;
-            shift[i] = x < n_cols && lse != -INFINITY ? -lse * kLog2e : -INFINITY;
+            // what gives nothing sits below slot 0 and sees nothing: its product may be NaN
+            t[i] = x < n_cols && lse != -INFINITY ? cr.slot0 + y / hpk : -1;
+            shift[i] = -lse * kLog2e;
         }
         const float scale_log2 = a.scale * kLog2e;
         const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
@@ -900,6 +901,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void score_tile_kernel
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kTileBytes];
     __shared__ __attribute__((aligned(16))) float shifts[2][QT];
     __shared__ __attribute__((aligned(16))) int slots[2][QT];
+    __shared__ int idle[2];  // whether a tile has columns that give nothing
     const PagedAttnArgs& a = b.at;
     const PagedKv& kv = a.kv;
     const int combo = blockIdx.x % geo.combos, rest = blockIdx.x / geo.combos, split = rest % geo.n_split;
@@ -936,14 +938,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void score_tile_kernel
         piece[i] = (p ^ (R::turn(c & 15) & (R::kPieces - 1))) << 4;
     }
     int si = (it0 * QT + lane) / hpk, sh = (it0 * QT + lane) % hpk;  // wave 0: the column whose lse it fetches
-    float lse_next = 0.f;
-    int slot_next = 0;
+    float shift_next = 0.f;
+    int slot_next = 0, idle_next = 0;
     auto load_tile = [&](int it, int buf) {
         const int base = min(it * QT / hpk, cr.n - 1);
         const T* q = uniform((const T*)a.q + (int64_t)(cr.row0 + base) * a.q_stride + (int64_t)kh * hpk * DH);
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-            const int x = min(ci[i], cr.n - 1);  // columns behind the last row: any that exist, they give nothing
+            const int x = min(ci[i], cr.n - 1);  // columns behind the last row: any that exist
             const uint32_t off = (uint32_t)((x - base) * (int)a.q_stride + ch[i] * DH) * (uint32_t)sizeof(T) + piece[i];
             dma_load16_at<false>(q, off, lds0 + buf * kTileBytes + wave * 1024, i * 4096);
             ci[i] += row_step, ch[i] += head_step;
@@ -952,17 +954,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void score_tile_kernel
         if (wave == 0) {
             const int x = min(si, cr.n - 1);
             const float lse = b.lse_in[(int64_t)(cr.row0 + x) * a.Hq + kh * hpk + sh];
-            lse_next = si < cr.n && lse != -INFINITY ? -lse * kLog2e : -INFINITY;
-            slot_next = cr.slot0 + x;
+            // a column behind the last row or with an lse of -infinity sits below slot 0 and sees nothing: its product may be NaN
+            const bool gives = si < cr.n && lse != -INFINITY;
+            shift_next = -lse * kLog2e;
+            slot_next = gives ? cr.slot0 + x : -1;
+            idle_next = __builtin_amdgcn_ballot_w64(!gives) != 0;
             si += row_step, sh += head_step;
             if (sh >= hpk) sh -= hpk, ++si;
         }
     };
     const float scale_log2 = a.scale * kLog2e;
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+    auto keep_next = [&](int buf) {
+        if (wave == 0) shifts[buf][lane] = shift_next, slots[buf][lane] = slot_next, idle[buf] = idle_next;
+    };
     if (it0 < it1) {
         load_tile(it0, 0);
-        if (wave == 0) shifts[0][lane] = lse_next, slots[0][lane] = slot_next;
+        keep_next(0);
     }
     for (int it = it0; it < it1; ++it) {
         const int buf = (it - it0) & 1;
@@ -974,7 +982,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void score_tile_kernel
         const int t_min = cr.slot0 + it * QT / hpk, t_max = cr.slot0 + min(cr.n - 1, (it * QT + QT - 1) / hpk);
         // rows of this tile that see any of the wave's tokens, and whether all see all
         const bool some = t_max >= tok0 && (!a.window || t_min - (tok1 - 1) < a.window || tok0 < a.sinks) && tok0 < len;
-        const bool all = t_min >= tok1 - 1 && (!a.window || t_max - tok0 < a.window || tok1 <= a.sinks);
+        const bool all = __builtin_amdgcn_readfirstlane(idle[buf]) == 0 && t_min >= tok1 - 1 && (!a.window || t_max - tok0 < a.window || tok1 <= a.sinks);
         if (some) {
 #pragma unroll
             for (int cg = 0; cg < QT / 16; ++cg) {
@@ -1007,7 +1015,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void score_tile_kernel
                 }
             }
         }
-        if (more && wave == 0) shifts[buf ^ 1][lane] = lse_next, slots[buf ^ 1][lane] = slot_next;
+        if (more) keep_next(buf ^ 1);
     }
     store_scores<MB>(b, geo, combo, split, ScoreSlot(b, combo, tok0, 16 * MB, len), tok0, gone, acc);
 }

@@ -138,3 +138,38 @@ def test_a_decode_loop_at_a_full_cache_leaves_it_alone():
         out, lse = _attend(c, q, cu, 1, Hq)
         assert torch.equal(out, want) and torch.equal(lse, want_lse)
     assert torch.equal(c.pool.view(torch.uint8), before.view(torch.uint8))
+
+
+@pytest.mark.parametrize("layout", [TINY, B128, B64, F128, B96], ids=ids)
+@pytest.mark.parametrize("new", [1, 8, 150])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 3)])
+def test_rows_whose_lse_is_minus_infinity_give_no_score_whatever_their_queries_hold(layout, new, window, sinks):
+    """Rows of a padded batch, say: lse -infinity, queries of NaN, infinities and numbers whose products overflow."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = layout
+    lens, news = [700, 160, 30], [new, new, min(new, 7)]
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=2)
+    q, cu, _ = _queries(news, Hq, dh, dtype, seed=3)
+    q, n = q.clone(), sum(news)
+    _, lse = _attend(c, q, cu, new, Hq, window, sinks)
+    dead = torch.zeros(n, Hq, dtype=torch.bool, device="cuda")
+    dead[::3] = dead[n - 1] = True                     # whole rows, the last one among them
+    dead[1::3, Hq - 1] = True                          # and single heads
+    lse[dead] = -float("inf")
+    bad = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device="cuda").to(q.dtype)
+    bad = bad[torch.arange(n * Hq, device="cuda") % 4].view(n, Hq, 1)
+    scores = []
+    for x in (torch.zeros_like(bad), bad):
+        rows = torch.where(dead[..., None], x, q.view(n, Hq, dh)).view(n, -1).contiguous()
+        need = rpo.rpo_kv_score_ws_bytes(c.dev, n, new, 700, Hq, window, sinks)
+        for use_ws in (False, True):
+            ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need and use_ws else None
+            score = torch.zeros(3, Hkv, 700, device="cuda")
+            rpo.rpo_kv_score(c.dev, rows, cu, new, lse, None, score, window, sinks, ws_dev=ws, max_len=700)
+            scores.append(score)
+    torch.cuda.synchronize()
+    assert all(bool(s.isfinite().all()) for s in scores)
+    assert torch.equal(scores[0], scores[2]) and torch.equal(scores[1], scores[3])
+    live = torch.where(dead, 0.0, 1.0).view(n, Hkv, -1).sum(dim=(0, 2)).tolist()
+    for h in range(Hkv):                               # every live row and head gives its weights, which add up to 1
+        assert abs(scores[3][:, h].double().sum().item() - live[h]) <= 1e-3 * live[h]
