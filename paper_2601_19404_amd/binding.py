@@ -457,10 +457,17 @@ class PagedKV:
         return self
 
 
+_TOO_LARGE = "a number does not fit 32 bits"
+
+
 # A decode step makes these calls layer by layer: their checks are kept to a few attribute reads (2.9 us of a call, of which
 # 1.3 are ctypes; 3.4 more are the launch).
-def _on(kv: PagedKV, stream, *tensors) -> int:
-    """The stream to launch on; the cache has to lie on the current device, and every tensor and the stream there too."""
+def _on(kv: PagedKV, stream, whole: int, *tensors) -> int:
+    """The stream to launch on; the cache has to lie on the current device, and every tensor and the stream there too.
+    whole: the call's whole numbers, or-ed together: ctypes would cut what does not fit 32 bits (the library refuses numbers
+    below 0 itself)."""
+    if whole >> 31 not in (0, -1):
+        raise ValueError(_TOO_LARGE)
     index = kv.index
     if torch._C._cuda_getDevice() != index:
         raise ValueError(f"the cache lies on cuda:{index}, which is not the current device")
@@ -528,12 +535,14 @@ def rpo_kv_append(kv: PagedKV, k_dev: torch.Tensor, v_dev: torch.Tensor, cu_rows
     if n != n2 or not width == width2 == kv.n_kv_heads * kv.head_dim:
         raise ValueError("k_dev and v_dev: need equally many rows of n_kv_heads * head_dim values")
     cu = _cu(cu_rows_dev, kv)
-    on = _on(kv, stream, k_dev, v_dev, cu_rows_dev)
+    on = _on(kv, stream, max_new, k_dev, v_dev, cu_rows_dev)
     _check(lib().rpo_kv_append(kv.ref, k_dev.data_ptr(), k_stride, v_dev.data_ptr(), v_stride, cu, n, max_new, on))
 
 
 def rpo_attn_paged_ws_bytes(kv: PagedKV, n_rows: int, max_new: int, max_len: int, n_q_heads: int, window: int = 0,
                             n_sinks: int = 0) -> int:
+    if (n_rows | max_new | max_len | n_q_heads | window | n_sinks) >> 31 not in (0, -1):
+        raise ValueError(_TOO_LARGE)
     return lib().rpo_attn_paged_ws_bytes(kv.ref, n_rows, max_new, max_len, n_q_heads, window, n_sinks)
 
 
@@ -549,14 +558,18 @@ def rpo_attn_paged(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, 
     lse = None if lse_out_dev is None else _floats(lse_out_dev, n * heads, "lse_out_dev")
     ws, ws_bytes = _workspace(ws_dev)
     cu = _cu(cu_rows_dev, kv)
-    on = _on(kv, stream, q_dev, out_dev, cu_rows_dev, lse_out_dev, ws_dev)
-    _check(lib().rpo_attn_paged(kv.ref, q_dev.data_ptr(), q_stride, cu, n, max_new,
-                                kv.capacity if max_len is None else max_len, heads, kv.scale if scale is None else scale,
-                                window, n_sinks, out_dev.data_ptr(), out_stride, lse, ws, ws_bytes, on))
+    if max_len is None:
+        max_len = kv.capacity
+    on = _on(kv, stream, max_new | max_len | window | n_sinks, q_dev, out_dev, cu_rows_dev, lse_out_dev, ws_dev)
+    _check(lib().rpo_attn_paged(kv.ref, q_dev.data_ptr(), q_stride, cu, n, max_new, max_len, heads,
+                                kv.scale if scale is None else scale, window, n_sinks, out_dev.data_ptr(), out_stride, lse, ws,
+                                ws_bytes, on))
 
 
 def rpo_kv_score_ws_bytes(kv: PagedKV, n_rows: int, max_new: int, max_len: int, n_q_heads: int, window: int = 0,
                           n_sinks: int = 0) -> int:
+    if (n_rows | max_new | max_len | n_q_heads | window | n_sinks) >> 31 not in (0, -1):
+        raise ValueError(_TOO_LARGE)
     return lib().rpo_kv_score_ws_bytes(kv.ref, n_rows, max_new, max_len, n_q_heads, window, n_sinks)
 
 
@@ -571,10 +584,12 @@ def rpo_kv_score(kv: PagedKV, q_dev: torch.Tensor, cu_rows_dev: torch.Tensor, ma
         raise ValueError("score_in_dev and score_out_dev differ in shape")
     ws, ws_bytes = _workspace(ws_dev)
     cu = _cu(cu_rows_dev, kv)
-    on = _on(kv, stream, q_dev, cu_rows_dev, lse_dev, score_in_dev, score_out_dev, ws_dev)
-    _check(lib().rpo_kv_score(kv.ref, q_dev.data_ptr(), q_stride, cu, n, max_new,
-                              kv.capacity if max_len is None else max_len, heads, kv.scale if scale is None else scale,
-                              window, n_sinks, lse, _ptr(score_in_dev), score_out_dev.data_ptr(), row, ws, ws_bytes, on))
+    if max_len is None:
+        max_len = kv.capacity
+    on = _on(kv, stream, max_new | max_len | window | n_sinks, q_dev, cu_rows_dev, lse_dev, score_in_dev, score_out_dev, ws_dev)
+    _check(lib().rpo_kv_score(kv.ref, q_dev.data_ptr(), q_stride, cu, n, max_new, max_len, heads,
+                              kv.scale if scale is None else scale, window, n_sinks, lse, _ptr(score_in_dev),
+                              score_out_dev.data_ptr(), row, ws, ws_bytes, on))
 
 
 def rpo_kv_evict(kv: PagedKV, score_dev: torch.Tensor, budget: int, n_sinks: int, n_recent: int, dst: PagedKV,
@@ -585,7 +600,7 @@ def rpo_kv_evict(kv: PagedKV, score_dev: torch.Tensor, budget: int, n_sinks: int
     for t, n, name in ((len_out_dev, kv.n_seqs, "len_out_dev"), (kept_out_dev, kv.n_seqs * kv.n_kv_heads * budget, "kept_out_dev")):
         if t.dtype is not torch.int32 or not t.is_contiguous() or t.numel() < n:
             raise ValueError(f"{name}: need at least {n} contiguous int32 values")
-    on = _on(kv, stream, score_dev, len_out_dev, kept_out_dev, score_out_dev, dst.lens)
+    on = _on(kv, stream, budget | n_sinks | n_recent, score_dev, len_out_dev, kept_out_dev, score_out_dev, dst.lens)
     _check(lib().rpo_kv_evict(kv.ref, score_dev.data_ptr(), row, budget, n_sinks, n_recent, dst.ref,
                               len_out_dev.data_ptr(), _ptr(score_out_dev), row_out, kept_out_dev.data_ptr(), on))
 

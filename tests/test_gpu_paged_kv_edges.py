@@ -173,3 +173,26 @@ def test_rows_whose_lse_is_minus_infinity_give_no_score_whatever_their_queries_h
     live = torch.where(dead, 0.0, 1.0).view(n, Hkv, -1).sum(dim=(0, 2)).tolist()
     for h in range(Hkv):                               # every live row and head gives its weights, which add up to 1
         assert abs(scores[3][:, h].double().sum().item() - live[h]) <= 1e-3 * live[h]
+
+
+def test_binding_refuses_numbers_that_32_bits_do_not_hold():
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = B128
+    c = Cache([100], Hkv, dh, pt, dtype, seed=1)
+    to = Cache([0], Hkv, dh, pt, dtype, seed=2, cap=64, stale=0.0)
+    q, cu, _ = _queries([2], Hq, dh, dtype, seed=1)
+    out, lse, score = torch.zeros_like(q), torch.zeros(2, Hq, device="cuda"), torch.zeros(1, Hkv, 100, device="cuda")
+    kept, big = torch.zeros(100, dtype=torch.int32, device="cuda"), 2 ** 32
+    before = c.pool.clone()
+    for call in (lambda: rpo.rpo_attn_paged(c.dev, q, cu, 2, out, big), lambda: rpo.rpo_attn_paged(c.dev, q, cu, 2, out, 5, big),
+                 lambda: rpo.rpo_attn_paged(c.dev, q, cu, big + 2, out), lambda: rpo.rpo_attn_paged(c.dev, q, cu, 2, out, max_len=big),
+                 lambda: rpo.rpo_kv_score(c.dev, q, cu, 2, lse, None, score, big),
+                 lambda: rpo.rpo_kv_score(c.dev, q, cu, big + 2, lse, None, score),
+                 lambda: rpo.rpo_kv_append(c.dev, q[:, :256], q[:, :256], cu, big + 2),
+                 lambda: rpo.rpo_kv_evict(c.dev, score, 50, big, 0, to.dev, to.dev.lens, kept),
+                 lambda: rpo.rpo_kv_evict(c.dev, score, 50, 0, big, to.dev, to.dev.lens, kept),
+                 lambda: rpo.rpo_kv_evict(c.dev, score, 50 - big, 0, 0, to.dev, to.dev.lens, kept)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert torch.all(out == 0) and torch.all(score == 0) and torch.equal(c.pool.view(torch.uint8), before.view(torch.uint8))

@@ -125,3 +125,16 @@ def test_binding_refuses_host_tensors():
     pool = torch.zeros(4, 2 * 2 * 16 * 32)
     with pytest.raises(ValueError):
         b.PagedKV(pool, torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 16, 2, 32)
+
+
+def test_binding_refuses_numbers_that_32_bits_do_not_hold():
+    """2^32 would reach the library as 0: no window, an empty cache."""
+    import types
+    kv = types.SimpleNamespace(ref=C.byref(_kv(n_seqs=1, table_stride=100)))
+    for size in (b.rpo_attn_paged_ws_bytes, b.rpo_kv_score_ws_bytes):
+        assert size(kv, 200, 200, 4000, 12) > 0 and size(kv, 200, 200, 4000, 12, 2 ** 31 - 1, 2 ** 31 - 1) > 0
+        for wrong in ((2 ** 32 + 200, 200, 4000, 12), (200, 200, 2 ** 32 + 4000, 12), (200, 200, 4000, 2 ** 32 + 12),
+                      (200, 200, 4000, 12, 2 ** 32), (200, 200, 4000, 12, 4, 2 ** 31), (200, -2 ** 32 + 200, 4000, 12)):
+            with pytest.raises(ValueError):
+                size(kv, *wrong)
+        assert size(kv, 200, 200, 4000, 12, -1) == 0               # below 0: the library's own refusal
