@@ -422,12 +422,16 @@ class PagedKV:
         _dev(lens, torch.int32, "lens")
         if table.dim() != 2 or lens.numel() < table.shape[0]:
             raise ValueError("table must be 2-D, lens [n_seqs]")
+        if min(page_tokens, n_kv_heads, head_dim) < 1 or max(page_tokens, n_kv_heads, head_dim) >> 31:
+            raise ValueError("page_tokens, n_kv_heads and head_dim must be 1 to 2^31 - 1")
         if pool[0].numel() < 2 * n_kv_heads * page_tokens * head_dim:
             raise ValueError("pool: a page is shorter than 2 x n_kv_heads x page_tokens x head_dim")
         if not pool.device == table.device == lens.device:
             raise ValueError("pool, table and lens lie on different devices")
         self.pool, self.table, self.lens = pool, table, lens
-        self.desc = PagedKvDesc(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), pool.stride(0), pool.shape[0],
+        # the stride of a single page is any number
+        page_stride = pool.stride(0) if pool.shape[0] > 1 else pool[0].numel()
+        self.desc = PagedKvDesc(pool.data_ptr(), table.data_ptr(), lens.data_ptr(), page_stride, pool.shape[0],
                                 table.shape[0], table.shape[1], page_tokens, n_kv_heads, head_dim,
                                 RPO_F32 if pool.dtype == torch.float32 else RPO_BF16)
         self._fill()

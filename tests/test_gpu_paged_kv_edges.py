@@ -196,3 +196,24 @@ def test_binding_refuses_numbers_that_32_bits_do_not_hold():
             call()
     torch.cuda.synchronize()
     assert torch.all(out == 0) and torch.all(score == 0) and torch.equal(c.pool.view(torch.uint8), before.view(torch.uint8))
+
+
+def test_binding_refuses_cache_sizes_below_one():
+    from paper_2601_19404_amd import binding as rpo
+    c = Cache([100], 2, 128, 64, "bf16", seed=1)
+    for pt, heads, dh in ((64, 2, 0), (64, 2, -128), (0, 2, 128), (64, -2, 128), (64, 2, 2 ** 32 + 128)):
+        with pytest.raises(ValueError):
+            rpo.PagedKV(c.pool, c.dev.table, c.dev.lens, pt, heads, dh)
+
+
+def test_a_pool_of_one_page_whose_stride_means_nothing():
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = B128
+    page = torch.zeros(2 * Hkv * pt * dh, dtype=torch.bfloat16, device="cuda")
+    pool = page.as_strided((1, page.numel()), (1, 1))
+    lens, table = torch.tensor([3], dtype=torch.int32).cuda(), torch.zeros(1, 1, dtype=torch.int32).cuda()
+    kv = rpo.PagedKV(pool, table, lens, pt, Hkv, dh)
+    q, cu, _ = _queries([3], Hq, dh, dtype, seed=1)
+    rpo.rpo_kv_append(kv, q[:, :256], q[:, 256:512], cu, 3)
+    torch.cuda.synchronize()
+    assert torch.equal(page[: 3 * dh].view(3, dh), q[:, :dh])
