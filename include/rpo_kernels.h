@@ -114,7 +114,8 @@ int rpo_kv_append(const rpo_paged_kv *kv, const void *k_dev, int64_t k_stride, c
  * the values, as in the batch's attention, and those of a chunk are divided by their sum as rounded, so that equal values come
  * out as they are.  A NaN or infinity in a slot reaches the rows that see it and may reach the rows
  * of the same sequence that are computed together with them; in slots that no row of the call sees it does nothing.
- * Errors: RPO_EINVAL, RPO_ENOMEM (ws_bytes), RPO_EHIP. */
+ * On the matrix cores n_seqs * n_kv_heads times the pieces of 64 or 128 of max_new * n_q_heads / n_kv_heads columns must stay
+ * below 2^24.  Errors: RPO_EINVAL, RPO_ENOMEM (ws_bytes), RPO_EHIP. */
 size_t rpo_attn_paged_ws_bytes(const rpo_paged_kv *kv, int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads,
                                int32_t window, int32_t n_sinks);
 int rpo_attn_paged(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, const int32_t *cu_rows_dev, int32_t n_rows,
@@ -129,7 +130,8 @@ int rpo_attn_paged(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, 
  *                 same array.  score_stride >= the longest cache (slots beyond it get no score); slots from len on are left
  *                 as they were.  The sums run in a fixed order: equal inputs give equal bits.
  *   ws_dev        as for rpo_attn_paged, rpo_kv_score_ws_bytes long
- * The other arguments as for rpo_attn_paged; slots from max_len on get no score.  Errors: RPO_EINVAL, RPO_ENOMEM, RPO_EHIP. */
+ * The other arguments as for rpo_attn_paged; slots from max_len on get no score.  n_seqs * n_kv_heads * max_len / 256 (fp32: 128)
+ * must stay below 2^24.  Errors: RPO_EINVAL, RPO_ENOMEM, RPO_EHIP. */
 size_t rpo_kv_score_ws_bytes(const rpo_paged_kv *kv, int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads,
                              int32_t window, int32_t n_sinks);
 int rpo_kv_score(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, const int32_t *cu_rows_dev, int32_t n_rows,
@@ -143,7 +145,7 @@ int rpo_kv_score(const rpo_paged_kv *kv, const void *q_dev, int64_t q_stride, co
  * which other sequences share stay as they are.  A shorter sequence goes over whole.
  *   score_dev     device fp32 [n_seqs, n_kv_heads, score_stride], score_stride >= the longest cache (tokens beyond it are
  *                 not looked at)
- *   budget        >= 1, >= n_sinks + n_recent, at most what a row of dst's table holds
+ *   budget        >= 1, >= n_sinks + n_recent, at most what a row of dst's table holds and 2^30 - 64
  *   dst           same n_seqs, n_kv_heads, head_dim and dtype as src; its len_dev is not read and may be NULL; no page that
  *                 its tables name may be one that src's name.  Slots beyond the kept ones are left as they were
  *   len_out_dev   device int32 [n_seqs]: min(len, budget); may be src's or dst's len_dev

@@ -403,6 +403,7 @@ struct PagedAttnArgs {
 };
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
 size_t paged_attn_ws_bytes(const PagedAttnArgs& a);  // pointers are not looked at
+bool paged_attn_fits(const PagedAttnArgs& a);        // whether one launch holds the call
 
 struct PagedScoreArgs {
     PagedAttnArgs at;        // out, lse unused
@@ -413,5 +414,6 @@ struct PagedScoreArgs {
 };
 hipError_t launch_paged_score(const PagedScoreArgs& a, hipStream_t s);
 size_t paged_score_ws_bytes(const PagedScoreArgs& a);
+bool paged_score_fits(const PagedScoreArgs& a);
 
 }  // namespace rpo

@@ -1134,7 +1134,7 @@ __global__ __launch_bounds__(256) void score_rows_kernel(PagedScoreArgs b) {
     }
 }
 
-constexpr int64_t kMaxGrid = 0xffffff;  // workgroups of 256 threads: a launch has fewer than 2^32 threads
+constexpr int64_t kMaxGrid = 0xffffff;  // workgroups of 256 threads: a launch has fewer than 2^32 threads in a row
 
 // Whether the matrix kernels take a call: fragments are 16 aligned bytes, offsets inside a tile of rows 32 bits.
 bool tiles_take(const PagedAttnArgs& a) {
@@ -1171,15 +1171,16 @@ int attn_splits(const PagedAttnArgs& a) {
     return (int)(n < 1 ? 1 : n < 64 ? n : 64);
 }
 
+// Workgroups that join a sequence's rows.
+int64_t join_groups(const PagedAttnArgs& a) { return ceil_div64((int64_t)a.max_new * a.Hq * (a.kv.dh / 4), 256); }
+
 template <typename T, int DH>
 hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
     TileGeom geo;
     geo.combos = a.kv.n_seqs * a.kv.Hkv;
     geo.n_split = a.ws ? attn_splits(a) : 1;
     geo.part = (float*)a.ws;
-    const int64_t grid = attn_tiles(a) * geo.combos * geo.n_split;
-    const int64_t join = ceil_div64((int64_t)a.max_new * a.Hq * (DH / 4), 256);
-    if (grid > kMaxGrid || join > kMaxGrid) return hipErrorInvalidValue;
+    const int64_t grid = attn_tiles(a) * geo.combos * geo.n_split, join = join_groups(a);
     const bool wide = (1 << a.kv.shift) >= 2 * Mat<T>::kGroup, small = tile_cols(a) == 64;
     auto tiles = [&](auto lse) {
         return wide ? (small ? attn_tile_kernel<T, DH, 1, true, lse.value> : attn_tile_kernel<T, DH, 2, true, lse.value>)
@@ -1222,7 +1223,6 @@ hipError_t launch_score_tiles(const PagedScoreArgs& b, hipStream_t s) {
     geo.n_split = a.ws ? score_splits(b) : 1;
     geo.part = (float*)a.ws;
     const int64_t grid = (int64_t)ceil_div(a.max_len, 64 * kScoreBlocks<T>) * geo.combos * geo.n_split;
-    if (grid > kMaxGrid) return hipErrorInvalidValue;
     if (few_take(a))
         score_few_kernel<T, DH><<<(unsigned)grid, 256, 0, s>>>(b, geo);
     else
@@ -1234,6 +1234,18 @@ hipError_t launch_score_tiles(const PagedScoreArgs& b, hipStream_t s) {
 }
 
 }  // namespace
+
+bool paged_attn_fits(const PagedAttnArgs& a) {
+    if (!tiles_take(a)) return true;  // its grid has three dimensions
+    const int n = a.ws ? attn_splits(a) : 1;
+    return attn_tiles(a) * a.kv.n_seqs * a.kv.Hkv * n <= kMaxGrid && (n == 1 || join_groups(a) <= kMaxGrid);
+}
+bool paged_score_fits(const PagedScoreArgs& b) {
+    const PagedAttnArgs& a = b.at;
+    if (!score_tiles_take(b)) return ceil_div(a.max_len, 32) <= kMaxGrid;
+    const int tokens = a.kv.dtype == kF32 ? 64 * kScoreBlocks<float> : 64 * kScoreBlocks<bf16>;
+    return (int64_t)ceil_div(a.max_len, tokens) * a.kv.n_seqs * a.kv.Hkv * (a.ws ? score_splits(b) : 1) <= kMaxGrid;
+}
 
 size_t paged_attn_ws_bytes(const PagedAttnArgs& a) {
     const int n = attn_splits(a);

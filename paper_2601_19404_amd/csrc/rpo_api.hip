@@ -1250,6 +1250,7 @@ namespace {
 
 constexpr int kMaxSeqs = 65535;  // grid dimensions y and z
 constexpr int kMaxNew = 1 << 26;  // workgroups of 64 threads along x: a launch has fewer than 2^32 threads
+constexpr int kMaxBudget = (1 << 30) - 64;  // workgroups of 256 threads for 64 tokens each
 
 // The checks of a cache that the host can make; fills in the kernels' form of it.
 int paged_kv(const char* who, const rpo_paged_kv* kv, bool needs_len, PagedKv* o) {
@@ -1403,6 +1404,7 @@ extern "C" int rpo_attn_paged(const rpo_paged_kv* kv, const void* q_dev, int64_t
     a.out = out_dev;
     a.out_stride = out_stride;
     a.lse = lse_out_dev;
+    if (!paged_attn_fits(a)) return fail(RPO_EINVAL, "rpo_attn_paged: more rows x heads x sequences than one launch holds");
     HIP_TRY(launch_paged_attn(a, (hipStream_t)stream));
     return RPO_OK;
 }
@@ -1430,6 +1432,7 @@ extern "C" int rpo_kv_score(const rpo_paged_kv* kv, const void* q_dev, int64_t q
     a.score_in = score_in_dev;
     a.score_out = score_out_dev;
     a.score_stride = score_stride;
+    if (!paged_score_fits(a)) return fail(RPO_EINVAL, "rpo_kv_score: more max_len x heads x sequences than one launch holds");
     HIP_TRY(launch_paged_score(a, (hipStream_t)stream));
     return RPO_OK;
 }
@@ -1446,6 +1449,7 @@ extern "C" int rpo_kv_evict(const rpo_paged_kv* src, const float* score_dev, int
         return fail(RPO_EINVAL, "rpo_kv_evict: src and dst differ in n_seqs, n_kv_heads, head_dim or dtype");
     if (n_sinks < 0 || n_recent < 0 || budget < 1 || (int64_t)n_sinks + n_recent > budget)
         return fail(RPO_EINVAL, "rpo_kv_evict: need budget >= 1 and >= n_sinks + n_recent, neither below 0");
+    if (budget > kMaxBudget) return fail(RPO_EINVAL, "rpo_kv_evict: budget must be at most %d", kMaxBudget);
     if (budget > ((int64_t)a.dst.table_stride << a.dst.shift))
         return fail(RPO_EINVAL, "rpo_kv_evict: dst's table does not hold the budget");
     if (score_stride < 1 || (score_out_dev && score_out_stride < budget))

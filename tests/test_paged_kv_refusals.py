@@ -138,3 +138,16 @@ def test_binding_refuses_numbers_that_32_bits_do_not_hold():
             with pytest.raises(ValueError):
                 size(kv, *wrong)
         assert size(kv, 200, 200, 4000, 12, -1) == 0               # below 0: the library's own refusal
+
+
+def test_what_one_launch_does_not_hold_is_refused_before_anything_is_enqueued():
+    many = dict(n_seqs=65535, n_kv_heads=1024, head_dim=32, page_stride=2 * 1024 * 64 * 32)
+    wide = dict(Hq=1024, q_stride=1024 * 32, out_stride=1024 * 32)
+    assert _attn(_kv(**many), **wide) == b.RPO_EINVAL and "one launch" in b.rpo_last_error()
+    assert _score(_kv(**many), **wide) == b.RPO_EINVAL and "one launch" in b.rpo_last_error()
+    long = dict(table_stride=1 << 24)                                  # 2^30 slots
+    assert _score(_kv(**long, n_seqs=8), max_len=1 << 30) == b.RPO_EINVAL and "one launch" in b.rpo_last_error()
+    odd = dict(long, head_dim=96, page_stride=2 * 2 * 64 * 96)          # the generic kernel: 32 slots a workgroup
+    assert _score(_kv(**odd), max_len=1 << 30) == b.RPO_EINVAL and "one launch" in b.rpo_last_error()
+    to = _kv(pool_dev=2 * P, len_dev=None, **long)
+    assert _evict(_kv(**long), to, budget=1 << 30) == b.RPO_EINVAL and "budget" in b.rpo_last_error()
