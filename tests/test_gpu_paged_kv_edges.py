@@ -217,3 +217,195 @@ def test_a_pool_of_one_page_whose_stride_means_nothing():
     rpo.rpo_kv_append(kv, q[:, :256], q[:, 256:512], cu, 3)
     torch.cuda.synchronize()
     assert torch.equal(page[: 3 * dh].view(3, dh), q[:, :dh])
+
+
+BAD_CU = [[0, 40, 80], [-3, 1, 2], [6, 2, 1 << 30], [9, 9, 9], [0, 3, -5], [-(1 << 31), (1 << 31) - 1, 8], [5, 8, 8]]
+
+
+def _ranges(cu, n_rows, max_new):
+    """(first row, rows of a call, rows by the range) of every sequence, as the kernels bound them."""
+    for a, b in zip(cu[:-1], cu[1:]):
+        n = 0 if a < 0 else max(0, min(min(b, n_rows) - a, max_new))
+        yield a, n, min(max(b - a, 0), 2 ** 31 - 1)
+
+
+@pytest.mark.parametrize("layout", [TINY, B128, B96], ids=ids)
+@pytest.mark.parametrize("cu", BAD_CU, ids=ids)
+def test_row_ranges_that_are_none_touch_no_other_row_slot_or_score(layout, cu):
+    """Row ranges that leave the arrays, run backwards or are longer than max_new: only rows that the arrays hold and that a
+    range names are computed, and nothing around the arrays is written."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = layout
+    S, T, n, most = 2, 100, 8, 4
+    c = Cache([T, T], Hkv, dh, pt, dtype, seed=1, stale=5.0)
+    q, _, _ = _queries([n], Hq, dh, dtype, seed=1)
+    dev = torch.tensor(cu, dtype=torch.int32).cuda()
+    named = torch.zeros(n + 4, dtype=torch.bool)
+    for a, k, _ in _ranges(cu, n, most):
+        if k:
+            named[2 + a: 2 + a + k] = True
+    for use_ws in (False, True):
+        guard = torch.full((n + 4, Hq * dh), 7.0, dtype=q.dtype, device="cuda")
+        lse = torch.full((n + 4, Hq), 7.0, device="cuda")
+        need = rpo.rpo_attn_paged_ws_bytes(c.dev, n, most, T, Hq) if use_ws else 0
+        ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda") if need else None
+        rpo.rpo_attn_paged(c.dev, q, dev, most, guard[2: 2 + n], lse_out_dev=lse[2: 2 + n], ws_dev=ws, max_len=T)
+        torch.cuda.synchronize()
+        assert torch.all(guard.cpu()[~named] == 7) and torch.all(lse.cpu()[~named] == 7)
+        assert not (guard.cpu()[named] == 7).all(dim=1).any() and (ws is None or torch.all(ws[need:] == 255))
+    score = torch.full((S + 2, Hkv, T + 5), 7.0, device="cuda")
+    rpo.rpo_kv_score(c.dev, q, dev, most, lse[2: 2 + n].clone(), None, score[1: 1 + S], max_len=T)
+    torch.cuda.synchronize()
+    assert torch.all(score[0] == 7) and torch.all(score[1 + S] == 7) and torch.all(score[:, :, T:] == 7)
+    want = c.pool.cpu().clone()
+    for s, (a, k, by_range) in enumerate(_ranges(cu, n, most)):
+        slots = torch.arange(T - by_range, T - by_range + k)
+        keep = slots >= 0
+        rows = q.cpu()[a: a + k][keep, : Hkv * dh].view(-1, Hkv, dh) if k else torch.zeros(0, Hkv, dh, dtype=q.dtype)
+        c.write(want, s, slots[keep], rows, rows)
+    rpo.rpo_kv_append(c.dev, q[:, : Hkv * dh], q[:, : Hkv * dh], dev, most)
+    torch.cuda.synchronize()
+    assert torch.equal(c.pool.cpu(), want)
+
+
+@pytest.mark.parametrize("budget", [10, 100, 395])
+def test_scores_of_kept_tokens_come_over_bit_for_bit(budget):
+    """Zeros of both signs, infinities, numbers below the normal range and NaN."""
+    from paper_2601_19404_amd import binding as rpo
+    values = torch.tensor([0.0, -0.0, 1.0, -1.0, float("inf"), float("-inf"), float("nan"), 1e-42, -1e-42, 3e38])
+    score = values[torch.randint(0, 10, (3, 2, 402), generator=torch.Generator().manual_seed(0))].cuda()
+    c = Cache([400, 399, 120], 2, 32, 16, "f32", seed=1)
+    to = Cache([0] * 3, 2, 32, 16, "f32", seed=2, cap=budget)
+    kept, got = torch.zeros(3, 2, budget, dtype=torch.int32, device="cuda"), torch.full((3, 2, budget + 2), 7.0, device="cuda")
+    rpo.rpo_kv_evict(c.dev, score, budget, 3, 4, to.dev, to.dev.lens, kept, got)
+    torch.cuda.synchronize()
+    for s in range(3):
+        for h in range(2):
+            slots = [j for j in kept[s, h].tolist() if j >= 0]
+            assert torch.equal(got[s, h, : len(slots)].view(torch.int32), score[s, h, slots].view(torch.int32))
+            assert torch.all(got[s, h, len(slots):] == 0)
+
+
+@pytest.mark.parametrize("T", [4095, 4096, 4097, 16384, 16385, 32768, 32769])
+def test_eviction_at_the_lengths_where_its_kernels_change(T):
+    from paper_2601_19404_amd import binding as rpo
+    budget, sinks, recent = 500, 4, 50
+    c = Cache([T], 1, 32, 64, "bf16", seed=1, cap=T)
+    to = Cache([0], 1, 32, 64, "bf16", seed=2, cap=budget, stale=0.0)
+    score = torch.round(4 * torch.rand(1, 1, T, generator=torch.Generator().manual_seed(T))) / 4
+    kept = torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda")
+    rpo.rpo_kv_evict(c.dev, score.cuda(), budget, sinks, recent, to.dev, to.dev.lens, kept)
+    assert kept[0, 0].tolist() == O.evict(score[0, 0].numpy().astype(np.float64), budget, sinks, recent)
+
+
+def test_eviction_into_free_pages_of_the_same_pool():
+    """Source and target share the pool and the array of lengths, as a program with one pool has it."""
+    from paper_2601_19404_amd import binding as rpo
+    _, Hkv, dh, dtype, pt = B128
+    lens, budget = [300, 65, 128], 70
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=1)
+    free = torch.cat([c.pool, torch.full((6, c.pool.shape[1]), 3.0, dtype=c.pool.dtype, device="cuda")])
+    n0 = c.pool.shape[0]
+    src = rpo.PagedKV(free, c.dev.table, c.dev.lens, pt, Hkv, dh)
+    table = torch.arange(n0, n0 + 6, dtype=torch.int32).view(3, 2).flip(0).contiguous()
+    dst = rpo.PagedKV(free, table.cuda(), c.dev.lens, pt, Hkv, dh)
+    score = torch.rand(3, Hkv, 300, generator=torch.Generator().manual_seed(1))
+    kept = torch.zeros(3, Hkv, budget, dtype=torch.int32, device="cuda")
+    rpo.rpo_kv_evict(src, score.cuda(), budget, 4, 16, dst, c.dev.lens, kept)
+    torch.cuda.synchronize()
+    assert torch.equal(free[:n0].view(torch.uint8), c.pool.view(torch.uint8)) and c.dev.lens.tolist() == [70, 65, 70]
+    want = torch.full((n0 + 6, c.pool.shape[1]), 3.0, dtype=c.pool.dtype)
+    c.table = table
+    for s, T in enumerate(lens):
+        for h in range(Hkv):
+            slots = O.evict(score[s, h, :T].numpy().astype(np.float64), budget, 4, 16)
+            c.write(want, s, torch.arange(len(slots)), c.k[s][slots, h], c.v[s][slots, h], h)
+    assert torch.equal(free[n0:].cpu(), want[n0:])
+
+
+@pytest.mark.parametrize("layout", [B128, F128], ids=ids)
+@pytest.mark.parametrize("new", [1, 150])
+def test_split_calls_are_captured_and_replayed(layout, new):
+    """Attention and scores with workspaces that they need, in one graph; the rows' inputs and the lengths change between the
+    replays, eager calls and another stream run in between: the eager results every time."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = layout
+    most = 3000
+    c = Cache([most, 2100], Hkv, dh, pt, dtype, seed=1)
+    q, cu, _ = _queries([new, new], Hq, dh, dtype, seed=1)
+    q = q.clone()
+    sizes = [f(c.dev, 2 * new, new, most, Hq) for f in (rpo.rpo_attn_paged_ws_bytes, rpo.rpo_kv_score_ws_bytes)]
+    assert sizes[0] > 0 and (new == 1 or sizes[1] > 0)
+    out, lse, score = torch.zeros_like(q), torch.zeros(2 * new, Hq, device="cuda"), torch.zeros(2, Hkv, most, device="cuda")
+
+    def work(ws):
+        rpo.rpo_attn_paged(c.dev, q, cu, new, out, lse_out_dev=lse, ws_dev=ws[0], max_len=most)
+        rpo.rpo_kv_score(c.dev, q, cu, new, lse, None, score, ws_dev=ws[1], max_len=most)
+
+    def run(call):
+        for t in (out, lse, score):
+            t.zero_()
+        call()
+        torch.cuda.synchronize()
+        return [t.clone() for t in (out, lse, score)]
+
+    spaces = [[torch.full((n,), 255, dtype=torch.uint8, device="cuda") if n else None for n in sizes] for _ in range(3)]
+    run(lambda: work(spaces[0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work(spaces[1])
+    for lens in ([3000, 2100], [700, 2100], [2999, 1], [3000, 2047]):
+        q.copy_(2 * torch.randn_like(q.float()))
+        c.dev.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        want = run(lambda: work(spaces[0]))
+        assert all(torch.equal(a, b) for a, b in zip(run(graph.replay), want)), lens
+
+        def aside():
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                work(spaces[2])
+        assert all(torch.equal(a, b) for a, b in zip(run(aside), want)), lens
+
+
+def test_a_captured_decode_step_goes_on_by_itself():
+    """Append, attention and scores of one step in a graph that counts the lengths up itself, replayed token after token."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = B128
+    start, steps = [60, 1000], 8
+    make = lambda: Cache([0, 0], Hkv, dh, pt, dtype, seed=1, cap=1100, stale=0.25)   # noqa: E731
+    rows = torch.randn(steps, 2, (Hq + 2 * Hkv) * dh, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    cu = torch.arange(3, dtype=torch.int32, device="cuda")
+    results = []
+    for captured in (False, True):
+        c = make()
+        c.dev.lens.copy_(torch.tensor(start, dtype=torch.int32))
+        row, out, lse = rows[0].clone(), torch.zeros(2, Hq * dh, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, Hq, device="cuda")
+        score = torch.zeros(2, Hkv, 1100, device="cuda")
+        need = rpo.rpo_attn_paged_ws_bytes(c.dev, 2, 1, 1100, Hq)
+        assert need > 0
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+        def step():
+            c.dev.lens.add_(1)
+            rpo.rpo_kv_append(c.dev, row[:, Hq * dh: (Hq + Hkv) * dh], row[:, (Hq + Hkv) * dh:], cu, 1)
+            rpo.rpo_attn_paged(c.dev, row[:, : Hq * dh], cu, 1, out, lse_out_dev=lse, ws_dev=ws, max_len=1100)
+            rpo.rpo_kv_score(c.dev, row[:, : Hq * dh], cu, 1, lse, score, score, max_len=1100)
+
+        call = step
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+            call = graph.replay
+        seen = []
+        for i in range(steps):
+            row.copy_(rows[i])
+            call()
+            torch.cuda.synchronize()
+            seen.append((out.clone(), lse.clone(), score.clone()))
+        assert c.dev.lens.tolist() == [n + steps for n in start]
+        results.append((seen, c.pool))
+    assert torch.equal(results[0][1], results[1][1])
+    for a, b in zip(results[0][0], results[1][0]):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))

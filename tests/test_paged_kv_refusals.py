@@ -151,3 +151,13 @@ def test_what_one_launch_does_not_hold_is_refused_before_anything_is_enqueued():
     assert _score(_kv(**odd), max_len=1 << 30) == b.RPO_EINVAL and "one launch" in b.rpo_last_error()
     to = _kv(pool_dev=2 * P, len_dev=None, **long)
     assert _evict(_kv(**long), to, budget=1 << 30) == b.RPO_EINVAL and "budget" in b.rpo_last_error()
+
+
+def test_a_workspace_that_is_too_small_is_refused_by_every_call_that_splits():
+    L, kv = b.lib(), _kv(n_seqs=1, table_stride=100)
+    for size, call, new in ((L.rpo_attn_paged_ws_bytes, _attn, 1), (L.rpo_attn_paged_ws_bytes, _attn, 200),
+                            (L.rpo_kv_score_ws_bytes, _score, 200)):
+        need = size(kv, new, new, 4000, 12, 0, 0)
+        assert need > 0
+        assert call(kv, n_rows=new, max_new=new, max_len=4000, ws=P, ws_bytes=need - 1) == b.RPO_ENOMEM
+        assert "%d needed" % need in b.rpo_last_error()
