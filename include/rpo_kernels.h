@@ -112,8 +112,8 @@ int rpo_kv_append(const rpo_paged_kv *kv, const void *k_dev, int64_t k_stride, c
  * bf16 and fp32 with head_dim 32, 64 or 128 and rows that start at multiples of 16 bytes run on the matrix cores, anything
  * else on a generic kernel.  Sums and statistics are fp32; with bf16 the weights p are rounded to bf16 before they multiply
  * the values, as in the batch's attention, and those of a chunk are divided by their sum as rounded, so that equal values come
- * out as they are.  A NaN or infinity in a slot reaches the rows that see it and may reach the rows
- * of the same sequence that are computed together with them; in slots that no row of the call sees it does nothing.
+ * out as they are.  A NaN or infinity in a slot reaches the rows that see it (in a value: its channel of
+ * theirs) and no others; rows that are computed together with such rows are computed once more, which takes longer.
  * On the matrix cores n_seqs * n_kv_heads times the pieces of 64 or 128 of max_new * n_q_heads / n_kv_heads columns must stay
  * below 2^24.  Errors: RPO_EINVAL, RPO_ENOMEM (ws_bytes), RPO_EHIP. */
 size_t rpo_attn_paged_ws_bytes(const rpo_paged_kv *kv, int32_t n_rows, int32_t max_new, int32_t max_len, int32_t n_q_heads,

@@ -63,6 +63,19 @@ struct Mat<bf16> {
     }
     // 16-byte unit of a values tile [octets][channels][8] that holds lane group g's tokens of group kk
     static __device__ inline int unit(int kk, int g, int dh, int ch) { return (4 * kk + g) * dh + ch; }
+    // dword d of an operand that holds 2 where bit i of bits is set and 0 elsewhere
+    static __device__ inline uint32_t twos(uint32_t bits, int d) {
+        return (bits >> (2 * d) & 1) * 0x4000u | (bits >> (2 * d + 1) & 1) * 0x40000000u;
+    }
+    // values without those that are not finite; up: the largest number where +infinity or NaN was, down: the smallest where
+    // -infinity or NaN was
+    static __device__ inline uint32_t finite(uint32_t x, uint32_t& up, uint32_t& down) {
+        constexpr uint32_t k1 = 0x00010001u;
+        const uint32_t odd = ((x & 0x7f807f80u) + 0x00800080u) >> 15 & k1, nan = ((x & 0x007f007fu) + 0x007f007fu) >> 7, neg = x >> 15;
+        up = (odd & (nan | ~neg)) * 0x7f7fu;
+        down = (odd & (nan | neg)) * 0xff7fu;
+        return x & ~(odd * 0xffffu);
+    }
 };
 template <>
 struct Mat<float> {
@@ -79,6 +92,13 @@ struct Mat<float> {
     static __device__ inline u32x4_t weights(const f32x4_t* s) { return __builtin_bit_cast(u32x4_t, s[0]); }
     static __device__ inline u32x4_t times(u32x4_t p, float f) { return __builtin_bit_cast(u32x4_t, __builtin_bit_cast(f32x4_t, p) * f); }
     static __device__ inline int unit(int kk, int g, int dh, int ch) { return ((2 * kk + (g >> 1)) * dh + ch) * 2 + (g & 1); }
+    static __device__ inline uint32_t twos(uint32_t bits, int d) { return (bits >> d & 1) * 0x40000000u; }
+    static __device__ inline uint32_t finite(uint32_t x, uint32_t& up, uint32_t& down) {
+        const uint32_t odd = ((x & 0x7f800000u) + 0x00800000u) >> 31, nan = ((x & 0x007fffffu) + 0x007fffffu) >> 23, neg = x >> 31;
+        up = (odd & (nan | ~neg)) * 0x7f7fffffu;
+        down = (odd & (nan | neg)) * 0xff7fffffu;
+        return x & (odd - 1);
+    }
 };
 
 // 16-byte pieces of a row, and where piece p of a row lies in LDS: permuted so that the 16 rows that a fragment reads at the
@@ -142,6 +162,102 @@ struct Span {
 
 // the lowest n bits (n below 0: none, above 32: all)
 __device__ inline uint32_t low_bits(int n) { return (uint32_t)((1ull << min(max(n, 0), 32)) - 1); }
+
+// A weight of 0 keeps a token from a row, but 0 times NaN or infinity is NaN: values that are not finite reach every column that
+// a wave computes with one that sees them.  A wave asks for that in the end, of its sums alone (a question in the loop, a product
+// of the values with zeros in every step that has a mask, cost 3 to 5 %): whether a column's sums are not finite though its
+// weights' sum is.
+template <int DH>
+__device__ inline bool only_values_not_finite(const f32x4_t (&ot)[DH / 16], float sum) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_fmaf(ot[i][e], 0.f, x);
+    return x != x && sum - sum == 0.f;
+}
+// Then it multiplies once more, the weights by what their sums are relative to, and without the values that are not finite:
+// those come in as products of the largest numbers with 2 for the columns that see them, which overflow to an infinity of
+// either sign; both make a NaN.  Straight from the pages, a step of M::kGroup tokens at a time, with no loads ahead: 4 x 4352
+// rows of 7B heads with NaN among the values 2.5 ms.  Without any, its registers cost the loops about 1 %: 576 -> 584 us.
+template <typename T, int DH, int NC, typename F>
+__device__ __forceinline__ void multiply_again(const PagedKv& kv, int s, int kh, const Span& span, int n_steps, F first_token,
+                                               const u32x4_t (&bq)[NC][Row<T, DH>::kFrags], const int (&limit)[NC],
+                                               const int (&from)[NC], float scale_log2, const float (&minus_ref)[NC],
+                                               f32x4_t (&ot)[NC][DH / 16]) {
+    using R = Row<T, DH>;
+    using M = Mat<T>;
+    constexpr int KS = M::kGroup, MB = KS / 16;
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, mask = (1 << kv.shift) - 1;
+    const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+    const u32x4_t none = {0, 0, 0, 0};
+    const T* const pool = (const T*)kv.pool;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) ot[c][i] = zero4;
+#pragma unroll 1
+    for (int x = 0; x < n_steps; ++x) {
+        const int tok = first_token(x);
+        int page[MB];
+        uint32_t there = 0;  // bit r: token r's page is
+#pragma unroll
+        for (int u = 0; u < MB; ++u) {
+            page[u] = tok + 16 * u < span.hi ? kv.page(s, tok + 16 * u) : -1;
+            there |= page[u] >= 0 ? 0xffffu << (16 * u) : 0u;
+        }
+        // what is not there is read from the first page, and cleared
+        f32x4_t sc[NC][MB];
+        {
+            const int r = M::token(0, c16), p = MB > 1 && r >> 4 ? page[MB - 1] : page[0];
+            const T* k = pool + kv.k_at(max(p, 0), kh) + (int64_t)((tok + r) & mask) * DH + g * R::kElems;
+            const uint32_t keep = ~(uint32_t)(p >> 31);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int j = 0; j < R::kFrags; ++j) {
+                    const u32x4_t a = *(const u32x4_t*)(k + (M::token(mb, 0) - M::token(0, 0)) * DH + 4 * j * R::kElems) & keep;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) sc[c][mb] = M::mma(a, bq[c][j], j == 0 ? zero4 : sc[c][mb]);
+                }
+        }
+        u32x4_t w[NC], view[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const uint32_t seen = low_bits(limit[c] - tok) & (low_bits(span.sinks - tok) | ~low_bits(from[c] - tok)) & there;
+            const uint32_t mine = seen >> (M::kLaneTok * g);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][mb][i], scale_log2, minus_ref[c]));
+                    sc[c][mb][i] = __uint_as_float(__float_as_uint(x) & (uint32_t)__builtin_amdgcn_sbfe((int)mine, M::token(mb, i), 1));
+                }
+            w[c] = M::weights(sc[c]);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) view[c][d] = M::twos(mine, d);
+        }
+        const int slot = tok + M::kLaneTok * g, p = MB > 1 && g >> 1 ? page[MB - 1] : page[0];
+        const T* v = pool + kv.v_at(max(p, 0), kh) + ((int64_t)((slot & mask) >> 3) * DH + c16) * 8 + (slot & 7);
+        const uint32_t keep = ~(uint32_t)(p >> 31);
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) {
+            u32x4_t a = *(const u32x4_t*)(v + 16 * 8 * i) & keep, ups, downs;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                uint32_t up, down;
+                a[d] = M::finite(a[d], up, down);
+                ups[d] = up, downs[d] = down;
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                // (each in a sum of its own: a product added to an infinity does not overflow before the sum does)
+                const f32x4_t high = M::mma(ups, view[c], zero4), low = M::mma(downs, view[c], zero4);
+                ot[c][i] = M::mma(a, w[c], ot[c][i]) + high + low;
+            }
+        }
+    }
+}
 
 // ---------------------------------------------------------------------------
 // chunks.  A wave multiplies every fragment that it reads from LDS with two column tiles (32 columns), which takes the LDS to
@@ -501,10 +617,21 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         clear_unseen(tok + KS, half_bits(gone, 1));
         add_values(p1);
     }
+    float total[NC], sum[NC];
+    bool again = false;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const float total = LSE ? sum_over_lane_groups(l[c]) : lr[c][0];
-        const float sum = kRounds ? lr[c][0] : total;
+        total[c] = LSE ? sum_over_lane_groups(l[c]) : lr[c][0];
+        sum[c] = kRounds ? lr[c][0] : total[c];
+        again |= only_values_not_finite<DH>(ot[c], sum[c]);
+    }
+    if (__builtin_amdgcn_ballot_w64(again) != 0) {
+        multiply_again<T, DH, NC>(
+            kv, s, kh, span, 2 * n, [&](int x) { return span.step_at(it0 + (x >> 1)) * KT + (x & 1) * KS; }, bq, limit, from, scale_log2,
+            minus_ref, ot);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
         int col = qt * kCols + (wave * NC + c) * 16 + c16;
         asm volatile("" : "+v"(col));  // worked out again rather than kept in registers for the whole loop
         if (col >= n_cols) continue;
@@ -512,18 +639,18 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
         const int head = kh * hpk + col % hpk;
         if (geo.n_split > 1) {
             const int64_t piece = (row * a.Hq + head) * geo.n_split + split;
-            if (g == 0) piece_sums<DH>(a, geo)[piece] = {sum != 0.f ? -minus_ref[c] : -INFINITY, sum, total, 0.f};
+            if (g == 0) piece_sums<DH>(a, geo)[piece] = {sum[c] != 0.f ? -minus_ref[c] : -INFINITY, sum[c], total[c], 0.f};
 #pragma unroll
             for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)(geo.part + piece * DH + 16 * i + 4 * g) = ot[c][i];
             continue;
         }
-        const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+        const float inv = sum[c] != 0.f ? 1.0f / sum[c] : 0.f;
         T* out = (T*)a.out + row * a.out_stride + (int64_t)head * DH;
 #pragma unroll
         for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[16 * i + 4 * g + e] = from_f32<T>(ot[c][i][e] * inv);
-        if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum != 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total) : -INFINITY;
+        if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum[c] != 0.f ? -minus_ref[c] * (1.0f / kLog2e) + logf(total[c]) : -INFINITY;
     }
 }
 
@@ -554,7 +681,8 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
     const bool real = c16 < n_cols;
     const int i_row = real ? c16 / hpk : 0, hq = kh * hpk + (real ? c16 % hpk : 0), t = cr.slot0 + i_row;
     const int limit = t + 1, from = a.window ? max(0, t - a.window + 1) : 0;
-    u32x4_t bq[R::kFrags];
+    u32x4_t cols[1][R::kFrags];
+    auto& bq = cols[0];
     {
         const T* q = (const T*)a.q + (int64_t)(cr.row0 + i_row) * a.q_stride + (int64_t)hq * DH;
 #pragma unroll
@@ -598,7 +726,8 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
                 v[i] = *(const u32x4_t*)(vp + (int64_t)(u0 + (sizeof(T) == 2 ? 16 : 32) * i) * R::kElems);
         }
     };
-    f32x4_t ot[DH / 16];
+    f32x4_t acc[1][DH / 16];
+    auto& ot = acc[0];
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i) ot[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
@@ -685,6 +814,13 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
     }
     // join the four waves
     const float wave_l = sum_over_lane_groups(l);
+    if (cr.n > 1 && __builtin_amdgcn_ballot_w64(only_values_not_finite<DH>(ot, wave_l)) != 0) {  // the columns of one row see the same
+        const int limits[1] = {limit}, froms[1] = {from};
+        const float minus_ref[1] = {m == -INFINITY ? 0.f : -m * scale_log2};
+        multiply_again<T, DH, 1>(
+            kv, s, kh, span, (it1 - it0 - wave + 3) >> 2, [&](int x) { return span.step_at(it0 + wave + 4 * x) * KS; }, cols, limits, froms,
+            scale_log2, minus_ref, acc);
+    }
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i) *(f32x4_t*)&os[wave][c16][16 * i + 4 * g] = ot[i];
     if (g == 0) ms[wave][c16] = m * scale_log2, ls[wave][c16] = wave_l;

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import paged_kv as O
-from tests.test_gpu_paged_kv import EPS, LAYOUTS, Cache, _check_attention, _check_score, _queries
+from tests.test_gpu_paged_kv import EPS, LAYOUTS, Cache, _queries, _tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -409,3 +409,48 @@ def test_a_captured_decode_step_goes_on_by_itself():
     assert torch.equal(results[0][1], results[1][1])
     for a, b in zip(results[0][0], results[1][0]):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("layout", [TINY, B128, B64, F128, B32, B96], ids=ids)
+@pytest.mark.parametrize("lens,new", [([130, 70], 2), ([130, 70], 60), ([1500, 900], 150), ([1500, 33], 2)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (25, 3)])
+def test_values_reach_the_rows_that_see_them_and_no_others(layout, lens, new, window, sinks):
+    """NaN and infinities in the values of tokens that some rows of a chunk see and others do not (the newest ones, and those that
+    leave the window): the others come out as the oracle has them without, the log-sum-exp and the other heads bit for bit."""
+    Hq, Hkv, dh, dtype, pt = layout
+    news = [new, min(new, 33)]
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=2)
+    q, cu, at = _queries(news, Hq, dh, dtype, seed=3)
+    clean = [_attend(c, q, cu, new, Hq, window, sinks, use_ws) for use_ws in (False, True)]
+    h, hpk = Hkv - 1, Hq // Hkv                                    # of the last KV head
+    refs, bad = [], []                                             # bad: (sequence, slot, channel, value)
+    for s, (T, n) in enumerate(zip(lens, news)):
+        rows = q[at[s]: at[s + 1]].float().cpu().numpy().reshape(n, Hq, dh)[:, h * hpk:]
+        refs.append(O.attention(rows, c.k[s][:, h:].float().numpy(), c.v[s][:, h:].float().numpy(), dh ** -0.5, window, sinks))
+        bad += [(s, T - 1, 1, np.nan), (s, T - n // 2 - 1, 0, -np.inf), (s, T - n // 2, 2, np.inf), (s, T - n // 2, 3, np.nan)]
+        leaves = T - n - window + 1 + n // 2                       # slot that only the first rows see
+        if window and leaves >= sinks:
+            bad += [(s, leaves, dh - 1, np.inf), (s, leaves, dh - 2, -np.inf)]
+    for s, j, d, x in bad:
+        v = c.v[s][j:j + 1].clone()
+        v[:, h, d] = float(x)
+        _rewrite(c, s, [j], v=v)
+    for (want, want_lse), use_ws in zip(clean, (False, True)):
+        out, lse = _attend(c, q, cu, new, Hq, window, sinks, use_ws)
+        assert torch.equal(lse, want_lse) and torch.equal(out[:, : h * hpk * dh], want[:, : h * hpk * dh])
+        for s, (T, n) in enumerate(zip(lens, news)):
+            ref, _, _, mag, big = refs[s]
+            got = out[at[s]: at[s + 1]].float().cpu().numpy().reshape(n, Hq, dh)[:, h * hpk:]
+            expect = np.zeros((n, dh))
+            t = np.arange(T - n, T)
+            for s2, j, d, x in bad:
+                if s2 == s:
+                    sees = (j <= t) & ((t - j < window) | (j < sinks) | (window == 0))
+                    with np.errstate(invalid="ignore"):
+                        expect[:, d] += np.where(sees, x, 0.0)
+            expect = np.broadcast_to(expect[:, None], got.shape)
+            odd = ~np.isfinite(expect)
+            np.testing.assert_array_equal(got[odd], expect[odd])
+            assert np.all(np.isfinite(got[~odd]))
+            off = np.abs(np.where(odd, 0.0, got) - np.where(odd, 0.0, ref)) - _tolerance(T, dh, ref, mag, big, dtype)
+            assert off[~odd].max() <= 0, (s, use_ws, off[~odd].max())
