@@ -380,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int p = __builtin_amdgcn_readfirstlane(raw[u]);
-            base[u] = p < 0 ? nullptr : pool + p * page_bytes + ((slot + 16 * u) & ((1 << kv.shift) - 1)) * R::kBytes;
+            base[u] = p < 0 ? nullptr : pool + p * page_bytes + (int64_t)((slot + 16 * u) & ((1 << kv.shift) - 1)) * R::kBytes;
         }
     };
     auto load_tile = [&](const char* const (&base)[U], bool values, uint32_t to) {

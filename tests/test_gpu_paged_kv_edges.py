@@ -454,3 +454,34 @@ def test_values_reach_the_rows_that_see_them_and_no_others(layout, lens, new, wi
             assert np.all(np.isfinite(got[~odd]))
             off = np.abs(np.where(odd, 0.0, got) - np.where(odd, 0.0, ref)) - _tolerance(T, dh, ref, mag, big, dtype)
             assert off[~odd].max() <= 0, (s, use_ws, off[~odd].max())
+
+
+@pytest.mark.parametrize("dtype,tokens", [("bf16", 1 << 24), ("f32", 1 << 23)])
+def test_pages_so_long_that_a_slots_offset_passes_32_bits(dtype, tokens):
+    """A cache in one page (two blocks of 4 GiB): rows at its end, whose keys and values lie more than 2^31 bytes into a block."""
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, near = 4, 1, 128, 300
+    small = Cache([near], Hkv, dh, 64, dtype, seed=3)
+    pool = torch.empty(1, 2 * tokens * dh, dtype=small.pool.dtype, device="cuda")
+    length = tokens - 77
+    lens, table = torch.tensor([length], dtype=torch.int32).cuda(), torch.zeros(1, 1, dtype=torch.int32).cuda()
+    kv = rpo.PagedKV(pool, table, lens, tokens, Hkv, dh)
+    k, v = (x[0].reshape(near, -1).cuda() for x in (small.k, small.v))
+    rpo.rpo_kv_append(kv, k, v, torch.tensor([0, near], dtype=torch.int32).cuda(), near)
+    for new in (1, 40):
+        q, cu, _ = _queries([new], Hq, dh, dtype, seed=5)
+        rows = q.float().cpu().numpy().reshape(new, Hq, dh)
+        ref, _, p, mag, big = O.attention(rows, small.k[0].float().numpy(), small.v[0].float().numpy(), dh ** -0.5, 100)
+        need = rpo.rpo_attn_paged_ws_bytes(kv, new, new, length, Hq, 100)
+        out, lse = torch.zeros_like(q), torch.zeros(new, Hq, device="cuda")
+        rpo.rpo_attn_paged(kv, q, cu, new, out, 100, lse_out_dev=lse, ws_dev=torch.empty(need, dtype=torch.uint8, device="cuda") if need else None,
+                           max_len=length)
+        score = torch.zeros(1, Hkv, length, device="cuda")
+        rpo.rpo_kv_score(kv, q, cu, new, lse, None, score, 100, max_len=length)
+        torch.cuda.synchronize()
+        off = np.abs(out.float().cpu().numpy().reshape(ref.shape) - ref) - _tolerance(near, dh, ref, mag, big, dtype)
+        assert off.max() <= 0, (new, off.max())
+        assert torch.all(score[:, :, : length - near] == 0)
+        w = O.score(p, Hkv)
+        rel = EPS * (2 * ((dh + 10) * big.max() + near + 16) + new * Hq + 16)      # as in the other tests of the scores
+        assert np.all(np.abs(score[0, :, length - near:].cpu().numpy() - w) <= rel * w + 2 * EPS * np.abs(w))
