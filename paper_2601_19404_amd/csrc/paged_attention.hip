@@ -264,16 +264,18 @@ __device__ __forceinline__ void multiply_again(const PagedKv& kv, int s, int kh,
 // half of the matrix units' time; 64 columns would need the registers of the second workgroup of a CU, whose waves fill each
 // other's gaps.  Direct loads leave the registers to the pipeline below; K is permuted on the way, V needs no permutation.
 // Bound by matrix and vector units about equally (products 1024 cycles, exponentials and their fma, sum and conversion 800
-// for a wave and a tile) and by what their taking turns leaves open: prefill of 4 x 4352 rows of 7B heads 542 us = 1.0 PFLOP/s,
-// with the log-sum-exp 564, where a large library product reaches 1.14.  One after the other in a tile 667 us; pipelined, fragments read just before
-// their products 613; read ahead 604; the maximum checked by lane and moved past 2^8 only 570; masks as bits, values
-// cleared in registers 545.
+// for a wave and a tile) and by what their taking turns leaves open: prefill of 4 x 4352 rows of 7B heads 555 to 580 us (by box
+// and clock) = 0.95 PFLOP/s, where a large library product reaches 1.12.  Steps, on the box of the time: one after the other in a
+// tile 667 us; pipelined, fragments read just before their products 613; read ahead 604; the maximum checked by lane and moved
+// past 2^8 only 570; masks as bits, values cleared in registers 545; the two sums below 563.
+// Registers: with 128 channels and 128 columns bf16 puts 24 to 42 of them away before the loop and fetches them behind it; fp32
+// fetches some of 44 to 46 in the loop, and so does bf16 with 32 channels on pages of 16 tokens (80 bytes a lane).
 // Weights are rounded to bf16 before they meet the values, which takes the matrix units' full rate; the output is divided by
 // the sum of the weights as they were rounded, so that it is a mean of the values with weights a little off and a row that sees
 // equal values (or one) returns them.  Divided by the unrounded sum it is off by the largest weight's rounding too: 1.4e-3
 // instead of 0 for rows that see one token, 2.3e-3 instead of 2.15e-3 over 512 to 4352 tokens, the result's own rounding 1.7e-3
-// among it.  That sum comes from a product with ones (as a sum of converted weights: 588 us, with the log-sum-exp), the
-// unrounded one, which the log-sum-exp needs, is added up only where it is asked for.
+// among it.  That sum comes from a product with ones (as a sum of converted weights 588 us), the unrounded one, which the
+// log-sum-exp needs, is added up only where it is asked for (563 us, without 543).
 // ---------------------------------------------------------------------------
 struct TileGeom {
     int combos;   // n_seqs * Hkv
@@ -657,7 +659,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(PagedAttnArgs a, Tile
 // ---------------------------------------------------------------------------
 // up to 16 query columns per KV head.  The keys and values are used once, so they go to registers directly; a wave has the
 // next step's 16 KiB on their way while it multiplies.  Bound by memory: 128 sequences of 4250 tokens of 7B heads 197 us =
-// 5.7 TB/s (a large copy moves 4.8 TB/s both ways together); one token over 2176 7.9 us, four rounds of dependent loads.
+// 5.7 TB/s (of 6.15 that a kernel which only reads reaches); one token over 2176 7.9 us, four rounds of dependent loads.
 // ---------------------------------------------------------------------------
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileGeom geo) {
@@ -856,7 +858,8 @@ __global__ __launch_bounds__(256, 2) void attn_few_kernel(PagedAttnArgs a, TileG
     }
 }
 
-// One workgroup per (row, heads): the pieces of a row's heads by their maxima.
+// A thread takes four channels of a head of a row of sequence blockIdx.y; threads are dealt to (row, head, channels) in order, so
+// that a workgroup may hold several rows, or parts of two.  Pieces are weighed by what their sums are relative to.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, TileGeom geo) {
     const int s = blockIdx.y, n_split = geo.n_split;
