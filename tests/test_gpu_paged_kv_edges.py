@@ -485,3 +485,21 @@ def test_pages_so_long_that_a_slots_offset_passes_32_bits(dtype, tokens):
         w = O.score(p, Hkv)
         rel = EPS * (2 * ((dh + 10) * big.max() + near + 16) + new * Hq + 16)      # as in the other tests of the scores
         assert np.all(np.abs(score[0, :, length - near:].cpu().numpy() - w) <= rel * w + 2 * EPS * np.abs(w))
+
+
+@pytest.mark.parametrize("layout", [TINY, B128, B64, F128, B96], ids=ids)
+@pytest.mark.parametrize("new", [1, 8, 150])
+@pytest.mark.parametrize("use_ws", [False, True])
+def test_outputs_do_not_depend_on_whether_the_lse_is_asked_for(layout, new, use_ws):
+    from paper_2601_19404_amd import binding as rpo
+    Hq, Hkv, dh, dtype, pt = layout
+    c = Cache([1500, 400], Hkv, dh, pt, dtype, seed=2)
+    q, cu, _ = _queries([new, new], Hq, dh, dtype, seed=3)
+    for window, sinks in ((0, 0), (700, 4)):
+        want, _ = _attend(c, q, cu, new, Hq, window, sinks, use_ws)
+        need = rpo.rpo_attn_paged_ws_bytes(c.dev, 2 * new, new, 1500, Hq, window, sinks) if use_ws else 0
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+        out = torch.full_like(want, 7.0)
+        rpo.rpo_attn_paged(c.dev, q, cu, new, out, window, sinks, ws_dev=ws, max_len=1500)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
