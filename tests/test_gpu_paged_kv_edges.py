@@ -13,6 +13,14 @@ TINY, B128, B64, F128, B32, B96 = LAYOUTS[0], LAYOUTS[1], LAYOUTS[3], LAYOUTS[4]
 ids = lambda x: "-".join(map(str, x))   # noqa: E731
 
 
+def _chunk_tolerance(T, dh, ref, mag, big, dtype):
+    """The bound of a chunk, whose bf16 weights are rounded in the products and in the sum that divides them.  With w_j (1 + d_j),
+    |d_j| <= 2^-8, in both, the quotient is off by sum p_j d_j (v_j - out) to first order, at most 2^-8 (sum p_j |v_j| + |out|):
+    2^-8 |out| more than with the exact sum, the second order within the factor 1 + 2^-7 as in _tolerance."""
+    more = 0.0 if dtype == "f32" else 2.0 ** -8 * np.abs(ref) * (1 + 2.0 ** -7)
+    return _tolerance(T, dh, ref, mag, big, dtype) + more
+
+
 def _attend(c, q, cu, most, Hq, window=0, sinks=0, use_ws=False, must_split=None):
     """(out, lse) of a call, with a workspace if asked for; must_split: whether the call has to need one."""
     from paper_2601_19404_amd import binding as rpo
@@ -59,6 +67,22 @@ def test_chunks_over_equal_values_return_the_value(layout, new, use_ws):
         else:
             off = (out.cpu() - want).abs() - (2 * max(lens) + 4) * EPS * want.abs()
             assert off.max() <= 0, (window, sinks, off.max())
+
+
+@pytest.mark.parametrize("layout", [B128, B64, B32, (32, 2, 128, "bf16", 256), (24, 3, 64, "bf16", 128)], ids=ids)
+@pytest.mark.parametrize("window,sinks", [(1, 1), (1, 4), (2, 0), (3, 2), (12, 0)])
+def test_chunks_over_a_few_visible_tokens_stay_within_their_roundings(layout, window, sinks):
+    """Where a few weights make the whole sum, their roundings do not even out."""
+    Hq, Hkv, dh, dtype, pt = layout
+    lens, news = [300, 160, 40], [150, 44, 40]
+    c = Cache(lens, Hkv, dh, pt, dtype, seed=window + sinks)
+    q, cu, at = _queries(news, Hq, dh, dtype, seed=7 * window + sinks)
+    out, _ = _attend(c, q, cu, max(news), Hq, window, sinks)
+    for s, (T, n) in enumerate(zip(lens, news)):
+        rows = q[at[s]: at[s + 1]].float().cpu().numpy().reshape(n, Hq, dh)
+        ref, _, _, mag, big = O.attention(rows, c.k[s].float().numpy(), c.v[s].float().numpy(), dh ** -0.5, window, sinks)
+        off = np.abs(out[at[s]: at[s + 1]].float().cpu().numpy().reshape(ref.shape) - ref)
+        assert (off - _chunk_tolerance(T, dh, ref, mag, big, dtype)).max() <= 0, s
 
 
 # new 1: the kernel for few rows, 40: the one for chunks; both are split over the tokens if there is a workspace
@@ -452,7 +476,7 @@ def test_values_reach_the_rows_that_see_them_and_no_others(layout, lens, new, wi
             odd = ~np.isfinite(expect)
             np.testing.assert_array_equal(got[odd], expect[odd])
             assert np.all(np.isfinite(got[~odd]))
-            off = np.abs(np.where(odd, 0.0, got) - np.where(odd, 0.0, ref)) - _tolerance(T, dh, ref, mag, big, dtype)
+            off = np.abs(np.where(odd, 0.0, got) - np.where(odd, 0.0, ref)) - _chunk_tolerance(T, dh, ref, mag, big, dtype)
             assert off[~odd].max() <= 0, (s, use_ws, off[~odd].max())
 
 
@@ -479,7 +503,7 @@ def test_pages_so_long_that_a_slots_offset_passes_32_bits(dtype, tokens):
         score = torch.zeros(1, Hkv, length, device="cuda")
         rpo.rpo_kv_score(kv, q, cu, new, lse, None, score, 100, max_len=length)
         torch.cuda.synchronize()
-        off = np.abs(out.float().cpu().numpy().reshape(ref.shape) - ref) - _tolerance(near, dh, ref, mag, big, dtype)
+        off = np.abs(out.float().cpu().numpy().reshape(ref.shape) - ref) - _chunk_tolerance(near, dh, ref, mag, big, dtype)
         assert off.max() <= 0, (new, off.max())
         assert torch.all(score[:, :, : length - near] == 0)
         w = O.score(p, Hkv)
